@@ -245,6 +245,140 @@ int conv3x3_tile_bwd(int N, int H, int W, int C_in, int C_out, const void *x_pad
                      size_t ws_bytes, void *stream);
 
 /* ====================================================================================
+ * A fully connected layer whose weights are split into E experts: every sample (token)
+ * goes through the k experts that its router prefers, and its k results are summed with
+ * their gates. One process's share, as above: w [E][d_out][ldw] holds one W_i per expert.
+ *
+ * The (token, expert) pairs are kept in EXPERT ORDER: pair by pair in the order of (expert,
+ * token, choice), each at its SLOT 0 .. offsets[E] - 1; expert e owns the slots
+ * offsets[e] .. offsets[e+1] - 1 (none, one or all of them). offsets, rows and slots are
+ * DEVICE int32 arrays, so no call waits for the GPU. Their values are not trusted: offsets
+ * are clamped to [0, n_rows] (an expert whose end lies before its start has no slots), and an
+ * index outside its array reads as zeros and writes nothing. One slot belongs to one expert
+ * and to one (token, choice): where offsets overlap or slots name a slot twice, the outputs
+ * there are undefined.
+ * Sizes: 1 <= E <= 512 and 1 <= k <= 16; the number of slots and of tokens below 2^31.
+ * ==================================================================================== */
+
+/* The router. logits [T][ldl] fp32, ldl >= E. Each token's k largest logits, in descending
+ * order, ties to the lowest expert: experts [T][k], and
+ *   gates[t][j] = exp(z_e) / sum exp(z)   over all E experts, or with renorm != 0 over the k
+ *                                         chosen ones.
+ * An expert whose logit is -inf is never chosen: where fewer than k are left (a padding
+ * token's row of -inf: none), experts[t][j] = -1, gates[t][j] = 0 and slots[t][j] = -1, and
+ * the pair has no slot. A NaN logit counts as the largest; it or +inf makes the row's gates
+ * NaN. Also the plan in expert order: offsets [E+1], rows [T*k] (the token of each slot;
+ * entries from offsets[E] on are left as they were) and slots [T][k] (each pair's slot).
+ * All outputs contiguous. T == 0 writes zeros to offsets only.
+ * ws (256-byte aligned): expert_route_workspace_bytes(T, E, k), which is 0 for sizes that
+ * expert_route refuses and may be 0 for others too (then ws is not read). */
+size_t expert_route_workspace_bytes(int T, int E, int k);
+int expert_route(int T, int E, int k, int renorm, const float *logits, int64_t ldl, float *gates,
+                 int32_t *experts, int32_t *offsets, int32_t *rows, int32_t *slots, void *ws,
+                 size_t ws_bytes, void *stream);
+
+/* The logits' gradient from the gates': dgates [T][k] contiguous, dlogits [T][lddl] fp32 (all E
+ * of a row are written). gates and experts as expert_route left them, logits the same input
+ * (read for renorm == 0 only, else it may be NULL). With p the softmax over all E,
+ *   renorm:  dz_e = sum_j [experts_j = e] g_j (dg_j - sum_i g_i dg_i)
+ *   else:    dz_e = sum_j [experts_j = e] g_j dg_j - p_e sum_i g_i dg_i
+ * A pair with experts[t][j] = -1 counts for nothing. */
+int expert_route_bwd(int T, int E, int k, int renorm, const float *logits, int64_t ldl,
+                     const float *gates, const int32_t *experts, const float *dgates,
+                     float *dlogits, int64_t lddl, void *stream);
+
+/* Every expert's forward product on its slots, y[s] = W_e x[rows[s]] + b_e, then ReLU if
+ * relu != 0, for the slots s of expert e. rows NULL: x is in expert order already (x[s],
+ * n_x == n_rows). n_rows: the number of rows of y (and of `rows`), at least offsets[E] if the
+ * offsets are to be served whole; rows of y that no expert owns are left as they were. n_x:
+ * the number of rows of x; a slot whose rows[s] is outside [0, n_x) reads a row of zeros.
+ * w: expert e's matrix at w + e*sw, [d_out][ldw], in dtype (sw >= (d_out-1)*ldw + d_in unless
+ * E == 1); bias [E][d_out] fp32 contiguous or NULL; x [n_x][ldx] in dtype; y [n_rows][ldy] in
+ * y_dtype. Sums in fp32, one rounding to y_dtype after bias and ReLU. */
+int expert_fwd(int dtype, int relu, int E, int d_out, int d_in, int n_rows, int n_x, const void *w,
+               int64_t ldw, int64_t sw, const float *bias, const void *x, int64_t ldx,
+               const int32_t *rows, const int32_t *offsets, void *y, int64_t ldy, int y_dtype,
+               void *stream);
+
+/* Their backward products, each skipped where its output is NULL (not all three):
+ *   dx[s]      = W_e^T dy[s]  (times [x[rows[s]] > 0] if mask_relu)   in expert order
+ *   dw_e[o][i] = sum over e's slots s of dy[s][o] x[rows[s]][i]
+ *   db_e[o]    = sum over e's slots s of dy[s][o]
+ * No factor 1/B: dy carries it. dy [n_rows][lddy] in dtype; x, rows, n_x, w as for expert_fwd
+ * (x may be NULL where neither dw nor mask_relu needs it, w where dx is NULL); dw expert by
+ * expert at dw + e*sdw, [d_out][lddw] fp32; db [E][d_out] fp32 contiguous; dx [n_rows][lddx] in
+ * dx_dtype. dw and db of an expert without slots are zero; rows of dx that no expert owns are
+ * left as they were. The gradient of x[t] itself is the sum of its slots' rows of dx:
+ * expert_combine with gates NULL. */
+int expert_bwd(int dtype, int E, int d_out, int d_in, int n_rows, int n_x, const void *w, int64_t ldw,
+               int64_t sw, const void *dy, int64_t lddy, const void *x, int64_t ldx,
+               const int32_t *rows, const int32_t *offsets, float *dw, int64_t lddw, int64_t sdw,
+               float *db, void *dx, int64_t lddx, int dx_dtype, int mask_relu, void *stream);
+
+/* Back to token order: y[t] = sum_j gates[t][j] ys[slots[t][j]] (gates NULL: 1), summed in fp32
+ * in the order of j. ys [n_rows][ldys] in dtype, y [T][ldy] in y_dtype, d columns; slots [T][k]
+ * and gates [T][k] contiguous; a slot outside [0, n_rows) adds nothing (whatever its gate). */
+int expert_combine(int dtype, int T, int k, int d, int n_rows, const void *ys, int64_t ldys,
+                   const int32_t *slots, const float *gates, void *y, int64_t ldy, int y_dtype,
+                   void *stream);
+
+/* Its backward pass: dys[slots[t][j]] = gates[t][j] dy[t] and dgates[t][j] = dy[t] . ys[slots[t][j]]
+ * (0 for a slot outside [0, n_rows)). dy [T][lddy], ys [n_rows][ldys] and dys [n_rows][lddys] in
+ * dtype; rows of dys that no slot names are left as they were. dgates [T][k] or NULL (then ys is
+ * not read). dys may not overlap ys. */
+int expert_combine_bwd(int dtype, int T, int k, int d, int n_rows, const void *dy, int64_t lddy,
+                       const void *ys, int64_t ldys, const int32_t *slots, const float *gates,
+                       void *dys, int64_t lddys, float *dgates, void *stream);
+
+/* ====================================================================================
+ * AdamW over many tensors in one launch: beside sgd_step, for gradients as mlp_bwd
+ * (fuse_sgd = 0) and expert_bwd store them.
+ * ==================================================================================== */
+
+/* One tensor of n >= 0 elements (all pointers to device memory, contiguous, aligned to their
+ * elements). */
+typedef struct {
+    float *w;           /* fp32 master weights */
+    uint16_t *w_lp;     /* bf16 copy of the updated weights, or NULL */
+    const void *grad;   /* gradient, in grad_dtype */
+    void *m, *v;        /* first and second moments: fp32, or one byte an element (state_bits 8) */
+    float *m_scale;     /* state_bits 8: ceil(n/256) scales each, one for every 256 elements from */
+    float *v_scale;     /* the tensor's first on; else unused */
+    int64_t n;
+    float decay;        /* weight decay, >= 0 */
+    int grad_dtype;     /* IMBD_F32 or IMBD_BF16 */
+    int state_bits;     /* 32 or 8 */
+} imbd_adamw_tensor;
+
+/* The plan of a set of tensors: adamw_plan writes it to HOST memory (plan_bytes from
+ * adamw_plan_bytes; 0 for a bad argument or a set without elements), the caller copies it to
+ * device memory (16-byte aligned) once and keeps both it and the tensors where they are. No two
+ * tensors of a set may share memory. */
+size_t adamw_plan_bytes(const imbd_adamw_tensor *tensors, int n_tensors);
+int adamw_plan(const imbd_adamw_tensor *tensors, int n_tensors, void *plan, size_t plan_bytes);
+
+/* One step t on all tensors of a plan. With g = grad_scale * grad, in fp32 with every product and
+ * sum rounded by itself:
+ *   m <- beta1 m + (1 - beta1) g          v <- beta2 v + (1 - beta2) g^2
+ *   w <- (1 - lr decay) w - lr/(1 - beta1^t) * m / (sqrt(v)/sqrt(1 - beta2^t) + eps)
+ *   w_lp <- bf16(w)
+ * (1 - beta, the bias corrections and 1 - lr*decay are formed in 64 bits.) t is `step` (>= 1), or
+ * with step_dev != NULL the device int32 that it points to: a captured launch then follows the
+ * caller's counter.
+ * State of 8 bits, in blocks of 256 elements: m is held as float8 e4m3 times m_scale =
+ * max|m| * (1/448) of the block, rounded to nearest; v as float8 e5m2 times v_scale =
+ * max v * (1/57344), rounded up or down by a dither of the element's index and t (a second moment
+ * that moves by 1 - beta2 a step would stay where it is if rounded to nearest), and never to zero:
+ * what is positive and under the smallest normal number is held as that number (2^-14). The update
+ * itself takes m and v before that rounding. A NaN or an infinity in a gradient makes the element's
+ * state NaN or infinite, and with 8-bit state its whole block's.
+ * plan_bytes and n_tensors as at adamw_plan; plan_bytes == 0 is a no-op. 0 <= beta < 1, eps >= 0,
+ * lr, eps and grad_scale finite. */
+int adamw_step(const void *plan, size_t plan_bytes, int n_tensors, double lr, double beta1,
+               double beta2, double eps, float grad_scale, int step, const int32_t *step_dev,
+               void *stream);
+
+/* ====================================================================================
  * Options: kernel routing and K splits (for A/B timing and for tests that force a
  * route; the defaults are the measured choices)
  * ==================================================================================== */
@@ -293,7 +427,9 @@ const char *imbd_option_name(int key);
 enum imbd_kernel_class {
     IMBD_K_GEMM_FWD = 0, IMBD_K_GEMM_DX = 1, IMBD_K_GEMM_DW = 2, IMBD_K_SPLITK = 3,
     IMBD_K_SOFTMAX = 4, IMBD_K_BIAS = 5, IMBD_K_SGD = 6, IMBD_K_CAST = 7,
-    IMBD_K_CONV_FWD = 8, IMBD_K_CONV_DGRAD = 9, IMBD_K_CONV_WGRAD = 10
+    IMBD_K_CONV_FWD = 8, IMBD_K_CONV_DGRAD = 9, IMBD_K_CONV_WGRAD = 10,
+    IMBD_K_EXPERT_FWD = 11, IMBD_K_EXPERT_DX = 12, IMBD_K_EXPERT_DW = 13,
+    IMBD_K_ROUTE = 14, IMBD_K_COMBINE = 15, IMBD_K_ADAMW = 16
 };
 /* Start recording HIP events around every launch of kernel class `cls` whose layer tag
  * equals `layer` (-1: any layer), up to max_launches launches. Creates the events

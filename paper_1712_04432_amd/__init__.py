@@ -15,10 +15,11 @@ import ctypes
 
 from ._abi import (IMBD_BF16, IMBD_F32, IMBD_K_BIAS, IMBD_K_CAST, IMBD_K_CONV_DGRAD,  # noqa: F401
                    IMBD_K_CONV_FWD, IMBD_K_CONV_WGRAD, IMBD_K_GEMM_DW, IMBD_K_GEMM_DX,
-                   IMBD_K_GEMM_FWD, IMBD_K_SGD, IMBD_K_SOFTMAX, IMBD_K_SPLITK, IMBD_OK,
+                   IMBD_K_GEMM_FWD, IMBD_K_SGD, IMBD_K_SOFTMAX, IMBD_K_SPLITK, IMBD_K_EXPERT_FWD,
+                   IMBD_K_EXPERT_DX, IMBD_K_EXPERT_DW, IMBD_K_ROUTE, IMBD_K_COMBINE, IMBD_K_ADAMW, IMBD_OK,
                    IMBD_EINVAL, IMBD_EUNSUPPORTED, IMBD_EHIP, IMBD_EWORKSPACE,
-                   IMBD_WS_ACT, IMBD_WS_DY, IMBD_WS_LOGITS, IMBD_WS_ROWLOSS, ImbdError, Layer,
-                   MlpDesc, check, load)
+                   IMBD_WS_ACT, IMBD_WS_DY, IMBD_WS_LOGITS, IMBD_WS_ROWLOSS, AdamWTensor, ImbdError,
+                   Layer, MlpDesc, check, load)
 from ._abi import IMBD_STATIC_SCRATCH_BYTES  # noqa: F401
 from ._abi import (IMBD_OPT_CONV_NT, IMBD_OPT_COUNT, IMBD_OPT_DW_GENERIC, IMBD_OPT_DW_STREAM,  # noqa: F401
                    IMBD_OPT_DW_WIDE_DUAL, IMBD_OPT_DW_WIDE_MIN_K, IMBD_OPT_LOCAL_PAIR, IMBD_OPT_GEMM_CFG, IMBD_OPT_GEMM_SPLITS, IMBD_OPT_SKINNY_OFF,
@@ -31,6 +32,8 @@ __all__ = [
     "mlp_local_bwd", "mlp_local_workspace_bytes", "conv3x3_tile_fwd", "conv3x3_tile_dgrad",
     "conv3x3_tile_wgrad", "conv3x3_tile_bwd", "conv3x3_wgrad_workspace_bytes", "timing_begin",
     "timing_end",
+    "expert_route_workspace_bytes", "expert_route", "expert_route_bwd", "expert_fwd", "expert_bwd",
+    "expert_combine", "expert_combine_bwd", "AdamW", "adamw_step",
     "ws_view", "dtype_code", "set_option", "get_option", "option_name", "options",
 ]
 
@@ -244,6 +247,233 @@ def conv3x3_tile_bwd(x_pad, w, dy_pad, dw, dx=None, ws=None, stream=None):
                                _ptr(dx), dtype_code(dx) if dx is not None else IMBD_BF16, _ptr(dw), _ptr(ws),
                                0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
           "conv3x3_tile_bwd")
+
+
+# ------------------------------------------------------------------- a layer of experts
+# These take their sizes from several tensors at once, and the kernels trust them, so the
+# tensors are checked against each other here (ValueError, TypeError); everything else is
+# checked by the library (ImbdError).
+def _sizes(t, shape, dtype, name, device, whole=False):
+    """Shape, type, device and layout of one tensor: rows without gaps between elements, or
+    (whole) contiguous."""
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple(shape)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: {t.dtype}, need {dtype}")
+    if t.device != device:
+        raise ValueError(f"{name}: on {t.device}, need {device}")
+    if not t.is_contiguous() and (whole or (t.shape[-1] > 1 and t.stride(-1) != 1)
+                                  or any(s < 0 for s in t.stride())):
+        raise ValueError(f"{name}: strides {t.stride()}")
+
+
+def _here(t, name):
+    """The tensor's device, which has to be the current one (the stream is taken from it)."""
+    if not t.is_cuda or t.device.index != _torch().cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, which is not the current device")
+    return t.device
+
+
+def _rows_ld(t):
+    """Leading dimension of a matrix, or of each matrix of a batch. (Of a single row, whose
+    stride means nothing, its length.)"""
+    return t.stride(-2) if t.shape[-2] > 1 else max(t.shape[-1], 1)
+
+
+def _float(t, name):
+    torch = _torch()
+    if t.dtype is not torch.bfloat16 and t.dtype is not torch.float32:
+        raise TypeError(f"{name}: {t.dtype}, need torch.bfloat16 or torch.float32")
+    return t.dtype
+
+
+def expert_route_workspace_bytes(T: int, E: int, k: int) -> int:
+    return load().expert_route_workspace_bytes(T, E, k)
+
+
+def expert_route(logits, gates, experts, offsets, rows, slots, ws=None, renorm: bool = True, stream=None):
+    """Each token's k experts (k = gates.shape[1]), their gates, and the plan in expert order."""
+    torch = _torch()
+    lib, dev = load(), _here(logits, "logits")
+    T, E = logits.shape
+    k = gates.shape[-1]
+    i32, f32 = torch.int32, torch.float32
+    _sizes(logits, (T, E), f32, "logits", dev)
+    _sizes(gates, (T, k), f32, "gates", dev, True)
+    _sizes(experts, (T, k), i32, "experts", dev, True)
+    _sizes(offsets, (E + 1,), i32, "offsets", dev, True)
+    _sizes(rows, (T * k,), i32, "rows", dev, True)
+    _sizes(slots, (T, k), i32, "slots", dev, True)
+    check(lib.expert_route(T, E, k, int(bool(renorm)), _ptr(logits), _rows_ld(logits), _ptr(gates), _ptr(experts),
+                           _ptr(offsets), _ptr(rows), _ptr(slots), _ptr(ws),
+                           0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "expert_route")
+
+
+def expert_route_bwd(logits, gates, experts, dgates, dlogits, renorm: bool = True, stream=None):
+    """The logits' gradient from the gates' (logits may be None with renorm)."""
+    torch = _torch()
+    lib, dev = load(), _here(dlogits, "dlogits")
+    T, E = dlogits.shape
+    k = gates.shape[-1]
+    f32 = torch.float32
+    _sizes(dlogits, (T, E), f32, "dlogits", dev)
+    if logits is not None:
+        _sizes(logits, (T, E), f32, "logits", dev)
+    _sizes(gates, (T, k), f32, "gates", dev, True)
+    _sizes(experts, (T, k), torch.int32, "experts", dev, True)
+    _sizes(dgates, (T, k), f32, "dgates", dev, True)
+    check(lib.expert_route_bwd(T, E, k, int(bool(renorm)), _ptr(logits), 0 if logits is None else _rows_ld(logits),
+                               _ptr(gates), _ptr(experts), _ptr(dgates), _ptr(dlogits), _rows_ld(dlogits),
+                               _stream(stream)), "expert_route_bwd")
+
+
+def expert_fwd(w, x, offsets, y, bias=None, relu: bool = False, rows=None, stream=None):
+    """y[s] = W_e x[rows[s]] + b_e, ReLU, for every slot s of every expert e. w [E][d_out][d_in]."""
+    torch = _torch()
+    lib, dev = load(), _here(w, "w")
+    E, d_out, d_in = w.shape
+    dt, ydt = _float(w, "w"), _float(y, "y")
+    n, n_x = y.shape[0], x.shape[0]
+    _sizes(w, (E, d_out, d_in), dt, "w", dev)
+    _sizes(x, (n_x, d_in), dt, "x", dev)
+    _sizes(y, (n, d_out), ydt, "y", dev)
+    _sizes(offsets, (E + 1,), torch.int32, "offsets", dev, True)
+    if bias is not None:
+        _sizes(bias, (E, d_out), torch.float32, "bias", dev, True)
+    if rows is not None:
+        _sizes(rows, (n,), torch.int32, "rows", dev, True)
+    check(lib.expert_fwd(dtype_code(dt), int(bool(relu)), E, d_out, d_in, n, n_x, _ptr(w), _rows_ld(w), w.stride(0),
+                         _ptr(bias), _ptr(x), _rows_ld(x), _ptr(rows), _ptr(offsets), _ptr(y), _rows_ld(y),
+                         dtype_code(ydt), _stream(stream)), "expert_fwd")
+
+
+def expert_bwd(w, dy, x, offsets, dw=None, db=None, dx=None, rows=None, mask_relu: bool = False, stream=None):
+    """The backward products of expert_fwd: dx in expert order, dw and db of every expert. What is
+    None is skipped; w gives the sizes also where dx is None."""
+    torch = _torch()
+    lib, dev = load(), _here(w, "w")
+    E, d_out, d_in = w.shape
+    dt, n = _float(w, "w"), dy.shape[0]
+    f32 = torch.float32
+    _sizes(w, (E, d_out, d_in), dt, "w", dev)
+    _sizes(dy, (n, d_out), dt, "dy", dev)
+    _sizes(offsets, (E + 1,), torch.int32, "offsets", dev, True)
+    n_x = n
+    if x is not None:
+        n_x = x.shape[0]
+        _sizes(x, (n_x, d_in), dt, "x", dev)
+    if rows is not None:
+        _sizes(rows, (n,), torch.int32, "rows", dev, True)
+    if dw is not None:
+        _sizes(dw, (E, d_out, d_in), f32, "dw", dev)
+    if db is not None:
+        _sizes(db, (E, d_out), f32, "db", dev, True)
+    if dx is not None:
+        _sizes(dx, (n, d_in), _float(dx, "dx"), "dx", dev)
+    check(lib.expert_bwd(dtype_code(dt), E, d_out, d_in, n, n_x, _ptr(w), _rows_ld(w), w.stride(0), _ptr(dy),
+                         _rows_ld(dy), _ptr(x), 0 if x is None else _rows_ld(x), _ptr(rows), _ptr(offsets), _ptr(dw),
+                         0 if dw is None else _rows_ld(dw), 0 if dw is None else dw.stride(0), _ptr(db), _ptr(dx),
+                         0 if dx is None else _rows_ld(dx), IMBD_F32 if dx is None else dtype_code(dx),
+                         int(bool(mask_relu)), _stream(stream)), "expert_bwd")
+
+
+def expert_combine(ys, slots, y, gates=None, stream=None):
+    """y[t] = sum_j gates[t][j] ys[slots[t][j]] (gates None: 1)."""
+    torch = _torch()
+    lib, dev = load(), _here(ys, "ys")
+    n, d = ys.shape
+    T, k = slots.shape
+    dt, ydt = _float(ys, "ys"), _float(y, "y")
+    _sizes(ys, (n, d), dt, "ys", dev)
+    _sizes(y, (T, d), ydt, "y", dev)
+    _sizes(slots, (T, k), torch.int32, "slots", dev, True)
+    if gates is not None:
+        _sizes(gates, (T, k), torch.float32, "gates", dev, True)
+    check(lib.expert_combine(dtype_code(dt), T, k, d, n, _ptr(ys), _rows_ld(ys), _ptr(slots), _ptr(gates), _ptr(y),
+                             _rows_ld(y), dtype_code(ydt), _stream(stream)), "expert_combine")
+
+
+def expert_combine_bwd(dy, ys, slots, gates, dys, dgates=None, stream=None):
+    """dys[slots[t][j]] = gates[t][j] dy[t] and dgates[t][j] = dy[t] . ys[slots[t][j]] (ys may be None
+    without dgates)."""
+    torch = _torch()
+    lib, dev = load(), _here(dy, "dy")
+    T, d = dy.shape
+    n, k = dys.shape[0], slots.shape[-1]
+    dt = _float(dy, "dy")
+    _sizes(dy, (T, d), dt, "dy", dev)
+    _sizes(dys, (n, d), dt, "dys", dev)
+    if ys is not None:
+        _sizes(ys, (n, d), dt, "ys", dev)
+    _sizes(slots, (T, k), torch.int32, "slots", dev, True)
+    _sizes(gates, (T, k), torch.float32, "gates", dev, True)
+    if dgates is not None:
+        _sizes(dgates, (T, k), torch.float32, "dgates", dev, True)
+    check(lib.expert_combine_bwd(dtype_code(dt), T, k, d, n, _ptr(dy), _rows_ld(dy), _ptr(ys),
+                                 0 if ys is None else _rows_ld(ys), _ptr(slots), _ptr(gates), _ptr(dys), _rows_ld(dys),
+                                 _ptr(dgates), _stream(stream)), "expert_combine_bwd")
+
+
+# ------------------------------------------------------------------------------- AdamW
+class AdamW:
+    """The plan of an AdamW update over many tensors, made once and kept.
+
+    tensors: sequence of dicts with w (fp32), grad (fp32 or bf16), m and v, and optionally w_lp
+    (bf16 copy) and decay (0). 32-bit state: m and v fp32. 8-bit state: m torch.float8_e4m3fn, v
+    torch.float8_e5m2, and m_scale and v_scale, fp32 [ceil(n/256)]. All contiguous, of one device,
+    and kept alive by the plan; no two may share memory. Zeros are the state before the first step.
+    """
+
+    def __init__(self, tensors):
+        torch = _torch()
+        lib = load()
+        tensors = [dict(t) for t in tensors]
+        self.tensors = tensors
+        arr = (AdamWTensor * max(len(tensors), 1))()
+        dev = _here(tensors[0]["w"], "w") if tensors else torch.device("cuda", torch.cuda.current_device())
+        f32 = torch.float32
+        for a, t in zip(arr, tensors):
+            w, n = t["w"], t["w"].numel()
+            bits8 = t["m"].dtype is torch.float8_e4m3fn
+            _sizes(w, w.shape, f32, "w", dev, True)
+            _sizes(t["grad"], w.shape, _float(t["grad"], "grad"), "grad", dev, True)
+            _sizes(t["m"], w.shape, torch.float8_e4m3fn if bits8 else f32, "m", dev, True)
+            _sizes(t["v"], w.shape, torch.float8_e5m2 if bits8 else f32, "v", dev, True)
+            if t.get("w_lp") is not None:
+                _sizes(t["w_lp"], w.shape, torch.bfloat16, "w_lp", dev, True)
+                a.w_lp = t["w_lp"].data_ptr()
+            if bits8:
+                blocks = ((n + 255) // 256,)
+                _sizes(t["m_scale"], blocks, f32, "m_scale", dev, True)
+                _sizes(t["v_scale"], blocks, f32, "v_scale", dev, True)
+                a.m_scale, a.v_scale = t["m_scale"].data_ptr(), t["v_scale"].data_ptr()
+            a.w, a.grad, a.m, a.v = w.data_ptr(), t["grad"].data_ptr(), t["m"].data_ptr(), t["v"].data_ptr()
+            a.n, a.decay = n, float(t.get("decay", 0.0))
+            a.grad_dtype, a.state_bits = dtype_code(t["grad"]), 8 if bits8 else 32
+        self.device = dev
+        self.n_tensors = len(tensors)
+        self.bytes = lib.adamw_plan_bytes(arr, len(tensors))
+        host = torch.empty(max(self.bytes, 8), dtype=torch.uint8)
+        # (a plan of no bytes: nothing to update, or a bad argument, which this call reports)
+        check(lib.adamw_plan(arr, len(tensors), _ptr(host), self.bytes), "adamw_plan")
+        self.plan = host.to(dev)
+
+
+def adamw_step(plan: AdamW, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step=1,
+               grad_scale: float = 1.0, stream=None):
+    """One AdamW step on every tensor of a plan. step: the step's number, from 1 on, or a device int32
+    tensor that holds it (read by the kernel, so a captured launch follows it)."""
+    lib = load()
+    if plan.device.index != _torch().cuda.current_device():
+        raise ValueError(f"plan: on {plan.device}, which is not the current device")
+    dev_step = None
+    if not isinstance(step, int):
+        _sizes(step, step.shape, _torch().int32, "step", plan.device, True)
+        if step.numel() != 1:
+            raise ValueError(f"step: {step.numel()} elements, need 1")
+        dev_step, step = _ptr(step), 1
+    check(lib.adamw_step(_ptr(plan.plan), plan.bytes, plan.n_tensors, float(lr), float(beta1), float(beta2),
+                         float(eps), float(grad_scale), step, dev_step, _stream(stream)), "adamw_step")
 
 
 def timing_begin(kernel_class: int, layer: int = -1, max_launches: int = 1000):

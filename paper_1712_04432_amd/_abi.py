@@ -17,7 +17,8 @@ IMBD_WS_ACT, IMBD_WS_LOGITS, IMBD_WS_DY, IMBD_WS_ROWLOSS = 0, 1, 2, 3
 IMBD_OPT_COUNT = 15
 IMBD_STATIC_SCRATCH_BYTES = 64 << 20
 (IMBD_K_GEMM_FWD, IMBD_K_GEMM_DX, IMBD_K_GEMM_DW, IMBD_K_SPLITK, IMBD_K_SOFTMAX, IMBD_K_BIAS,
- IMBD_K_SGD, IMBD_K_CAST, IMBD_K_CONV_FWD, IMBD_K_CONV_DGRAD, IMBD_K_CONV_WGRAD) = range(11)
+ IMBD_K_SGD, IMBD_K_CAST, IMBD_K_CONV_FWD, IMBD_K_CONV_DGRAD, IMBD_K_CONV_WGRAD, IMBD_K_EXPERT_FWD,
+ IMBD_K_EXPERT_DX, IMBD_K_EXPERT_DW, IMBD_K_ROUTE, IMBD_K_COMBINE, IMBD_K_ADAMW) = range(17)
 
 # every function the header declares: name -> (restype, argtypes)
 _i, _l, _p, _f, _d, _z = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_double, ctypes.c_size_t
@@ -30,6 +31,11 @@ class MlpDesc(ctypes.Structure):
 
 class Layer(ctypes.Structure):
     _fields_ = [("w", _p), ("w_lp", _p), ("b", _p), ("dw", _p), ("db", _p)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [("w", _p), ("w_lp", _p), ("grad", _p), ("m", _p), ("v", _p), ("m_scale", _p), ("v_scale", _p),
+                ("n", _l), ("decay", _f), ("grad_dtype", _i), ("state_bits", _i)]
 
 
 _PD = ctypes.POINTER(MlpDesc)
@@ -58,6 +64,17 @@ SIGNATURES = {
     "conv3x3_tile_wgrad": (_i, [_i, _i, _i, _i, _i, _p, _p, _p, _p, _z, _p]),
     "conv3x3_wgrad_workspace_bytes": (_z, [_i, _i, _i, _i, _i]),
     "conv3x3_tile_bwd": (_i, [_i, _i, _i, _i, _i, _p, _p, _p, _p, _i, _p, _p, _z, _p]),
+    "expert_route_workspace_bytes": (_z, [_i, _i, _i]),
+    "expert_route": (_i, [_i, _i, _i, _i, _p, _l, _p, _p, _p, _p, _p, _p, _z, _p]),
+    "expert_route_bwd": (_i, [_i, _i, _i, _i, _p, _l, _p, _p, _p, _p, _l, _p]),
+    "expert_fwd": (_i, [_i, _i, _i, _i, _i, _i, _i, _p, _l, _l, _p, _p, _l, _p, _p, _p, _l, _i, _p]),
+    "expert_bwd": (_i, [_i, _i, _i, _i, _i, _i, _p, _l, _l, _p, _l, _p, _l, _p, _p, _p, _l, _l, _p, _p, _l, _i, _i,
+                        _p]),
+    "expert_combine": (_i, [_i, _i, _i, _i, _i, _p, _l, _p, _p, _p, _l, _i, _p]),
+    "expert_combine_bwd": (_i, [_i, _i, _i, _i, _i, _p, _l, _p, _l, _p, _p, _p, _l, _p, _p]),
+    "adamw_plan_bytes": (_z, [ctypes.POINTER(AdamWTensor), _i]),
+    "adamw_plan": (_i, [ctypes.POINTER(AdamWTensor), _i, _p, _z]),
+    "adamw_step": (_i, [_p, _z, _i, _d, _d, _d, _d, _f, _i, _p, _p]),
     "imbd_set_option": (_i, [_i, _i]),
     "imbd_get_option": (_i, [_i, ctypes.POINTER(ctypes.c_int)]),
     "imbd_option_name": (ctypes.c_char_p, [_i]),

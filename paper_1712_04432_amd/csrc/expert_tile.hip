@@ -1,0 +1,321 @@
+// Products of an expert layer for any sizes, strides and alignments, fp32 and bf16: the kernel behind
+// expert_fwd and expert_bwd wherever the large-tile kernels do not take the call.
+//   forward  y[s][o]    = sum_i W_e[o][i] x[rows[s]][i]   (+ b_e[o], ReLU)     over the slots s of e
+//   Delta_X  dx[s][i]   = sum_o W_e[o][i] dy[s][o]        (* [x > 0])
+//   Delta_W  dw_e[o][i] = sum_s dy[s][o] x[rows[s]][i]    for every e; db_e[o] = sum_s dy[s][o]
+// Written as D(m, n) = sum_k A(m, k) B(k, n) with m the output's contiguous index:
+//   forward: m = o, n = s, k = i (both operands k-contiguous); Delta_X: m = i, n = s, k = o (W by k-rows);
+//   Delta_W: m = i, n = o, k = s (both by k-rows).
+//
+// A workgroup of four waves owns a 64 x 64 tile of D and walks K in steps of 128 bytes a row,
+// double-buffered in LDS with the next step's loads in flight over the products; rows of 144 bytes make
+// every fragment one conflict-free 16-byte read. Operands stored by k-rows are transposed in registers on
+// their way. Loads are 16 bytes at any element alignment, the chunks that an edge cuts go element by
+// element, and addresses are 64-bit, so no size or stride is special. fp32 operands run on the fp32 matrix
+// instruction: products and sums are fp32 for both types.
+
+#include "expert.h"
+
+namespace imbd {
+namespace {
+
+constexpr int XT = 64;          // tile side
+constexpr int XT_PITCH = 144;   // bytes per LDS row
+constexpr int XT_STAGE = 2 * XT * XT_PITCH;
+constexpr int XT_OUT = XT + 4;  // staging row pitch in floats
+static_assert(XT * XT_OUT * 4 <= 2 * XT_STAGE, "the staged tile reuses the operand buffers");
+
+// 16 bytes from p; elements at index >= valid read as 0.
+template <typename T>
+__device__ __forceinline__ u32x4 chunk16(const T *p, int valid) {
+  constexpr int VEC = 16 / (int)sizeof(T);
+  if (valid >= VEC) return *reinterpret_cast<const u32x4_any *>(p);
+  T tmp[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) tmp[e] = e < valid ? p[e] : T(0);
+  u32x4 r;
+  __builtin_memcpy(&r, tmp, 16);
+  return r;
+}
+
+// k-contiguous operand: 64 rows x 128 bytes, two chunks a thread. row(r) gives row r's first element, or
+// null for a row of zeros; it does not change over k.
+template <typename T>
+struct KcTile {
+  static constexpr int VEC = 16 / (int)sizeof(T);
+  const T *p[2];
+  u32x4 v[2];
+  template <typename F>
+  __device__ __forceinline__ void init(F row, int tid) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p[i] = row((tid + 256 * i) >> 3);
+  }
+  __device__ __forceinline__ void load(int k0, int K, int tid) {
+    const int kk = k0 + (tid & 7) * VEC;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v[i] = p[i] && kk < K ? chunk16<T>(p[i] + kk, K - kk) : u32x4{0u, 0u, 0u, 0u};
+  }
+  __device__ __forceinline__ void store(char *lds, int tid) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      *reinterpret_cast<u32x4 *>(lds + ((tid + 256 * i) >> 3) * XT_PITCH + (tid & 7) * 16) = v[i];
+  }
+};
+
+// Operand stored by k-rows: 128 bytes of k x 64 columns, in blocks of VEC x VEC transposed in registers
+// (bf16: the first 64 threads, fp32: the first 128; `tid` is rotated so that two such operands use
+// different waves). krow(k) gives the first column of the tile in k-row k, or null for zeros.
+template <typename T>
+struct TrTile {
+  static constexpr int VEC = 16 / (int)sizeof(T);
+  static constexpr int NB = 8 * XT / VEC;
+  u32x4 v[VEC];
+  template <typename F>
+  __device__ __forceinline__ void load(F krow, int k0, int K, int cols, int tid) {
+    if (tid >= NB) return;
+    const int kb = k0 + (tid & 7) * VEC, c = (tid >> 3) * VEC;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const T *p = kb + j < K && c < cols ? krow(kb + j) : nullptr;
+      v[j] = p ? chunk16<T>(p + c, cols - c) : u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+  __device__ __forceinline__ void store(char *lds, int tid) {
+    if (tid >= NB) return;
+#pragma unroll
+    for (int r = 0; r < VEC; ++r) {
+      u32x4 o;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if constexpr (VEC == 8) {
+          const uint32_t x = v[2 * q][r >> 1], y = v[2 * q + 1][r >> 1];
+          o[q] = (r & 1) ? ((x >> 16) | (y & 0xffff0000u)) : ((x & 0xffffu) | (y << 16));
+        } else {
+          o[q] = v[q][r];
+        }
+      }
+      *reinterpret_cast<u32x4 *>(lds + ((tid >> 3) * VEC + r) * XT_PITCH + (tid & 7) * 16) = o;
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ bool positive(T v) {
+  if constexpr (sizeof(T) == 2) return bf16_to_f32(v) > 0.f;
+  else return v > 0.f;
+}
+
+template <typename T, int PASS>
+__global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int tiles_m, int tiles_n) {
+  constexpr int VEC = 16 / (int)sizeof(T);
+  constexpr int BK = 8 * VEC;
+  __shared__ __attribute__((aligned(16))) char smem[2 * XT_STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+
+  // each XCD takes a contiguous range of the launch order; column tiles run fastest, so that the tiles
+  // that share rows of x (or dy) follow each other
+  int bid = blockIdx.x;
+  if ((gridDim.x & 7) == 0) bid = (bid & 7) * (int)(gridDim.x >> 3) + (bid >> 3);
+  const int tm = bid % tiles_m;
+  int e, n0, n_end, r0 = 0, K;
+  if constexpr (PASS == EXPERT_DW) {
+    const int t = bid / tiles_m;
+    e = t / tiles_n;
+    if (e >= a.E) return;
+    n0 = (t - e * tiles_n) * XT;
+    n_end = a.d_out;
+    expert_range(a, e, &r0, &K);
+  } else {
+    if (!find_row_tile<XT>(a, bid / tiles_m, &e, &n0, &n_end)) return;
+    K = PASS == EXPERT_FWD ? a.d_in : a.d_out;
+  }
+  const int m0 = tm * XT, M = PASS == EXPERT_FWD ? a.d_out : a.d_in;
+  const T *w = reinterpret_cast<const T *>(a.w) + (int64_t)e * a.sw;
+  const T *x = reinterpret_cast<const T *>(a.x);
+  const T *dy = reinterpret_cast<const T *>(a.dy);
+  auto x_row = [&](int s) -> const T * {
+    const int r = a.rows ? a.rows[s] : s;
+    return r >= 0 && r < a.n_x ? x + (int64_t)r * a.ldx : nullptr;
+  };
+
+  KcTile<T> ka, kb;
+  TrTile<T> ta, tb;
+  const int tid_b = tid ^ 128;  // (the k-row operand of n: the other half of the workgroup)
+  if constexpr (PASS == EXPERT_FWD) {
+    ka.init([&](int r) { return m0 + r < M ? w + (int64_t)(m0 + r) * a.ldw : nullptr; }, tid);
+    kb.init([&](int r) { return n0 + r < n_end ? x_row(n0 + r) : nullptr; }, tid);
+  } else if constexpr (PASS == EXPERT_DX) {
+    kb.init([&](int r) { return n0 + r < n_end ? dy + (int64_t)(n0 + r) * a.lddy : nullptr; }, tid);
+  }
+  auto load = [&](int k0) {
+    if constexpr (PASS == EXPERT_FWD) ka.load(k0, K, tid);
+    if constexpr (PASS != EXPERT_DW) kb.load(k0, K, tid);
+    if constexpr (PASS == EXPERT_DX) ta.load([&](int k) { return w + (int64_t)k * a.ldw + m0; }, k0, K, M - m0, tid);
+    if constexpr (PASS == EXPERT_DW) {
+      ta.load([&](int k) { const T *p = x_row(r0 + k); return p ? p + m0 : nullptr; }, k0, K, M - m0, tid);
+      tb.load([&](int k) { return dy + (int64_t)(r0 + k) * a.lddy + n0; }, k0, K, n_end - n0, tid_b);
+    }
+  };
+  auto store = [&](char *buf) {
+    if constexpr (PASS == EXPERT_FWD) ka.store(buf, tid);
+    else ta.store(buf, tid);
+    if constexpr (PASS != EXPERT_DW) kb.store(buf + XT * XT_PITCH, tid);
+    else tb.store(buf + XT * XT_PITCH, tid_b);
+  };
+
+  const int wm = (wave & 1) * 32, wn = (wave >> 1) * 32, fr = lane & 15, fg = lane >> 4;
+  f32x4 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const bool do_db = PASS == EXPERT_DW && a.db && tm == 0;
+  float dbsum = 0.f;
+
+  const int nk = (K + BK - 1) / BK;
+  if (nk > 0) {
+    load(0);
+    store(smem);
+  }
+  __syncthreads();
+  for (int kt = 0; kt < nk; ++kt) {
+    const char *sa = smem + (kt & 1) * XT_STAGE, *sb = sa + XT * XT_PITCH;
+    if (kt + 1 < nk) load((kt + 1) * BK);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      u32x4 fa[2], fb[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fa[i] = *reinterpret_cast<const u32x4 *>(sa + (wm + 16 * i + fr) * XT_PITCH + kk * 64 + fg * 16);
+        fb[i] = *reinterpret_cast<const u32x4 *>(sb + (wn + 16 * i + fr) * XT_PITCH + kk * 64 + fg * 16);
+      }
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fa[i]),
+                                                                __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const f32x4 af = __builtin_bit_cast(f32x4, fa[i]), bf = __builtin_bit_cast(f32x4, fb[j]);
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(af[q], bf[q], acc[i][j], 0, 0, 0);
+            }
+      }
+    }
+    if (do_db) {
+      // a quarter (two chunks) of row tid/4 of the dy tile, in the order of k
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const u32x4 q = *reinterpret_cast<const u32x4 *>(sb + (tid >> 2) * XT_PITCH + ((tid & 3) * 2 + c) * 16);
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int h = 0; h < 8; ++h) dbsum += bf16_to_f32((uint16_t)(q[h >> 1] >> (16 * (h & 1))));
+        } else {
+          const f32x4 f = __builtin_bit_cast(f32x4, q);
+#pragma unroll
+          for (int h = 0; h < 4; ++h) dbsum += f[h];
+        }
+      }
+    }
+    if (kt + 1 < nk) store(smem + ((kt + 1) & 1) * XT_STAGE);
+    __syncthreads();
+  }
+  if (do_db) {
+    dbsum += __shfl_xor(dbsum, 1, 64);
+    dbsum += __shfl_xor(dbsum, 2, 64);
+    if ((tid & 3) == 0 && n0 + (tid >> 2) < n_end) a.db[(int64_t)e * a.d_out + n0 + (tid >> 2)] = dbsum;
+  }
+  if (PASS == EXPERT_DW && !a.out) return;
+
+  // ---- the tile through LDS as [n][m], then rows of four outputs a thread
+  float *stg = reinterpret_cast<float *>(smem);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      *reinterpret_cast<f32x4 *>(stg + (wn + 16 * j + fr) * XT_OUT + wm + 16 * i + 4 * fg) = acc[i][j];
+  __syncthreads();
+  const int m = m0 + (tid & 15) * 4, cnt = min(4, M - m);
+  if (cnt <= 0) return;
+  float bias[4] = {0.f, 0.f, 0.f, 0.f};
+  if (PASS == EXPERT_FWD && a.bias) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (q < cnt) bias[q] = a.bias[(int64_t)e * a.d_out + m + q];
+  }
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int nl = 16 * p + (tid >> 4), n = n0 + nl;
+    if (n >= n_end) continue;
+    f32x4 v = *reinterpret_cast<const f32x4 *>(stg + nl * XT_OUT + (tid & 15) * 4);
+    if constexpr (PASS == EXPERT_FWD) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v[q] += bias[q];
+        if (a.relu) v[q] = v[q] < 0.f ? 0.f : v[q];  // (a NaN stays one)
+      }
+    }
+    if constexpr (PASS == EXPERT_DX) {
+      if (a.mask) {
+        const T *mk = x_row(n);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (!(mk && q < cnt && positive<T>(mk[m + q]))) v[q] = 0.f;
+      }
+    }
+    const int64_t at = (PASS == EXPERT_DW ? (int64_t)e * a.so : 0) + (int64_t)n * a.ldo + m;
+    if (a.out_dtype == IMBD_BF16) {
+      uint16_t *o = reinterpret_cast<uint16_t *>(a.out) + at;
+      if (cnt == 4) *reinterpret_cast<u32x2_any *>(o) = u32x2{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
+      else
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (q < cnt) o[q] = f32_to_bf16(v[q]);
+    } else {
+      float *o = reinterpret_cast<float *>(a.out) + at;
+      if (cnt == 4) *reinterpret_cast<f32x4_any *>(o) = v;
+      else
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (q < cnt) o[q] = v[q];
+    }
+  }
+}
+
+}  // namespace
+
+int run_expert_tile(int pass, int dtype, const ExpertArgs &a, hipStream_t s) {
+  const int M = pass == EXPERT_FWD ? a.d_out : a.d_in;
+  const int64_t tm = (M + XT - 1) / XT, tn = (a.d_out + XT - 1) / XT;
+  // (without dw, the first column of tiles alone sums db)
+  const int64_t cols = pass == EXPERT_DW && !a.out ? 1 : tm;
+  const int64_t blocks = (pass == EXPERT_DW ? a.E * tn : row_tiles_most(a.n_rows, a.E, XT)) * cols;
+  if (blocks >= ((int64_t)1 << 31) - 8) {
+    set_error("expert product: %lld tiles are more than one launch takes", (long long)blocks);
+    return IMBD_EUNSUPPORTED;
+  }
+  if (blocks == 0) return IMBD_OK;
+  const dim3 grid((unsigned)((blocks + 7) / 8 * 8)), wg(256);
+  const int cm = (int)cols, cn = (int)tn;
+  {
+    LaunchTimer t(IMBD_K_EXPERT_FWD + pass, 0, s);
+    if (dtype == IMBD_BF16) {
+      if (pass == EXPERT_FWD) hipLaunchKernelGGL((expert_tile_kernel<uint16_t, EXPERT_FWD>), grid, wg, 0, s, a, cm, cn);
+      else if (pass == EXPERT_DX) hipLaunchKernelGGL((expert_tile_kernel<uint16_t, EXPERT_DX>), grid, wg, 0, s, a, cm, cn);
+      else hipLaunchKernelGGL((expert_tile_kernel<uint16_t, EXPERT_DW>), grid, wg, 0, s, a, cm, cn);
+    } else {
+      if (pass == EXPERT_FWD) hipLaunchKernelGGL((expert_tile_kernel<float, EXPERT_FWD>), grid, wg, 0, s, a, cm, cn);
+      else if (pass == EXPERT_DX) hipLaunchKernelGGL((expert_tile_kernel<float, EXPERT_DX>), grid, wg, 0, s, a, cm, cn);
+      else hipLaunchKernelGGL((expert_tile_kernel<float, EXPERT_DW>), grid, wg, 0, s, a, cm, cn);
+    }
+  }
+  return check_launch("expert_tile");
+}
+
+}  // namespace imbd

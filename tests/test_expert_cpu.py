@@ -1,0 +1,151 @@
+"""Refusals of the expert layer's and AdamW's entry points, on the host: no device is touched."""
+import ctypes
+
+import numpy as np
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_1712_04432_amd as m
+    return m.load()
+
+
+P = ctypes.c_void_p(256)
+OK, EINVAL, EUNSUPPORTED, EWORKSPACE = 0, -1, -2, -4
+
+
+def _route(lib, T=1000, E=8, k=2, renorm=1, logits=P, ldl=8, gates=P, experts=P, offsets=P, rows=P, slots=P, ws=P,
+           ws_bytes=1 << 20):
+    return lib.expert_route(T, E, k, renorm, logits, ldl, gates, experts, offsets, rows, slots, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(T=-1), EINVAL), (dict(E=0), EINVAL), (dict(k=0), EINVAL), (dict(k=9), EINVAL),
+    (dict(E=513, ldl=513), EUNSUPPORTED), (dict(E=32, ldl=32, k=17), EUNSUPPORTED), (dict(T=2 ** 30, k=2), EUNSUPPORTED),
+    (dict(logits=None), EINVAL), (dict(gates=None), EINVAL), (dict(experts=None), EINVAL), (dict(offsets=None), EINVAL),
+    (dict(rows=None), EINVAL), (dict(slots=None), EINVAL), (dict(ldl=7), EINVAL),
+    (dict(ws=None), EWORKSPACE), (dict(ws_bytes=8), EWORKSPACE), (dict(ws=ctypes.c_void_p(264)), EINVAL)])
+def test_route_refuses(lib, bad, code):
+    assert _route(lib, **bad) == code
+    assert lib.imbd_last_error()
+
+
+def test_route_workspace(lib):
+    assert lib.expert_route_workspace_bytes(-1, 8, 2) == 0
+    assert lib.expert_route_workspace_bytes(16, 513, 2) == 0
+    sizes = [lib.expert_route_workspace_bytes(T, 64, 8) for T in (1, 1000, 16384, 1 << 20, 1 << 26)]
+    assert sizes[0] == 0 and sizes[1] > 0 and max(sizes) <= 256 * 64 * 4
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(T=-1), EINVAL), (dict(k=9), EINVAL), (dict(E=600, lddl=600, ldl=600), EUNSUPPORTED), (dict(logits=None), EINVAL),
+    (dict(logits=None, renorm=1), None), (dict(gates=None), EINVAL), (dict(experts=None), EINVAL),
+    (dict(dgates=None), EINVAL), (dict(dlogits=None), EINVAL), (dict(ldl=7), EINVAL), (dict(lddl=7), EINVAL)])
+def test_route_bwd_refuses(lib, bad, code):
+    a = dict(T=100, E=8, k=2, renorm=0, logits=P, ldl=8, gates=P, experts=P, dgates=P, dlogits=P, lddl=8)
+    a.update(bad)
+    if code is None:
+        a["T"] = 0  # (allowed: nothing to do)
+        code = OK
+    assert lib.expert_route_bwd(*a.values(), None) == code
+
+
+FWD = dict(dtype=1, relu=0, E=4, d_out=64, d_in=32, n_rows=10, n_x=5, w=P, ldw=32, sw=2048, bias=None, x=P, ldx=32, rows=P,
+           offsets=P, y=P, ldy=64, y_dtype=1)
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(dtype=2), EINVAL), (dict(y_dtype=-1), EINVAL), (dict(E=0), EINVAL), (dict(E=513), EUNSUPPORTED),
+    (dict(d_out=0), EINVAL), (dict(d_in=-3), EINVAL), (dict(n_rows=-1), EINVAL), (dict(n_x=-1), EINVAL),
+    (dict(w=None), EINVAL), (dict(x=None), EINVAL), (dict(offsets=None), EINVAL), (dict(y=None), EINVAL),
+    (dict(ldw=31), EINVAL), (dict(sw=2047), EINVAL), (dict(ldx=31), EINVAL), (dict(ldy=63), EINVAL),
+    (dict(rows=None), EINVAL), (dict(n_rows=0, y=None, x=None, n_x=0), OK),
+    (dict(n_rows=2 ** 31 - 1, n_x=2 ** 31 - 1, rows=None, d_out=2 ** 30, ldy=2 ** 30, sw=2 ** 40), EUNSUPPORTED)])
+def test_fwd_refuses(lib, bad, code):
+    assert lib.expert_fwd(*{**FWD, **bad}.values(), None) == code
+
+
+BWD = dict(dtype=1, E=4, d_out=64, d_in=32, n_rows=10, n_x=5, w=P, ldw=32, sw=2048, dy=P, lddy=64, x=P, ldx=32, rows=P,
+           offsets=P, dw=P, lddw=32, sdw=2048, db=P, dx=P, lddx=32, dx_dtype=1, mask_relu=1)
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(dtype=2), EINVAL), (dict(dx_dtype=7), EINVAL), (dict(E=513), EUNSUPPORTED), (dict(d_out=0), EINVAL),
+    (dict(dw=None, db=None, dx=None), EINVAL), (dict(offsets=None), EINVAL), (dict(dy=None), EINVAL),
+    (dict(x=None), EINVAL), (dict(x=None, dw=None), EINVAL), (dict(w=None), EINVAL), (dict(ldw=31), EINVAL),
+    (dict(sw=5), EINVAL), (dict(lddy=63), EINVAL), (dict(ldx=31), EINVAL), (dict(lddw=31), EINVAL), (dict(sdw=2047), EINVAL),
+    (dict(lddx=31), EINVAL), (dict(rows=None), EINVAL)])
+def test_bwd_refuses(lib, bad, code):
+    assert lib.expert_bwd(*{**BWD, **bad}.values(), None) == code
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(dtype=2), EINVAL), (dict(y_dtype=2), EINVAL), (dict(T=-1), EINVAL), (dict(k=0), EINVAL),
+    (dict(k=17), EUNSUPPORTED), (dict(d=0), EINVAL), (dict(n_rows=-1), EINVAL), (dict(ys=None), EINVAL),
+    (dict(slots=None), EINVAL), (dict(y=None), EINVAL), (dict(ldys=31), EINVAL), (dict(ldy=31), EINVAL), (dict(T=0), OK)])
+def test_combine_refuses(lib, bad, code):
+    a = dict(dtype=1, T=10, k=2, d=32, n_rows=20, ys=P, ldys=32, slots=P, gates=None, y=P, ldy=32, y_dtype=1)
+    a.update(bad)
+    assert lib.expert_combine(*a.values(), None) == code
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(dtype=2), EINVAL), (dict(T=-1), EINVAL), (dict(k=17), EUNSUPPORTED), (dict(d=0), EINVAL), (dict(dy=None), EINVAL),
+    (dict(slots=None), EINVAL), (dict(gates=None), EINVAL), (dict(dys=None), EINVAL), (dict(ys=None), EINVAL),
+    (dict(lddy=31), EINVAL), (dict(ldys=31), EINVAL), (dict(lddys=31), EINVAL), (dict(T=0), OK)])
+def test_combine_bwd_refuses(lib, bad, code):
+    a = dict(dtype=1, T=10, k=2, d=32, n_rows=20, dy=P, lddy=32, ys=P, ldys=32, slots=P, gates=P, dys=P, lddys=32, dgates=P)
+    a.update(bad)
+    assert lib.expert_combine_bwd(*a.values(), None) == code
+
+
+def _tensor(**kw):
+    from paper_1712_04432_amd import AdamWTensor
+    a = dict(w=4096, w_lp=None, grad=8192, m=12288, v=16384, m_scale=None, v_scale=None, n=1000, decay=0.0, grad_dtype=0,
+             state_bits=32)
+    a.update(kw)
+    return AdamWTensor(*a.values())
+
+
+def _array(*ts):
+    from paper_1712_04432_amd import AdamWTensor
+    return (AdamWTensor * len(ts))(*ts)
+
+
+@pytest.mark.parametrize("bad", [dict(n=-1), dict(grad_dtype=3), dict(state_bits=16), dict(decay=-0.5),
+                                 dict(decay=float("nan")), dict(decay=float("inf")), dict(w=None), dict(grad=None),
+                                 dict(m=None), dict(v=None), dict(state_bits=8), dict(state_bits=8, m_scale=64)])
+def test_adamw_plan_refuses(lib, bad):
+    arr = _array(_tensor(), _tensor(**bad))
+    assert lib.adamw_plan_bytes(arr, 2) == 0
+    assert lib.adamw_plan(arr, 2, P, 1 << 20) == EINVAL
+
+
+def test_adamw_plan(lib):
+    """The plan covers every tensor once, whatever their sizes, and tensors of no elements cost nothing."""
+    assert lib.adamw_plan_bytes(None, 0) == 0 and lib.adamw_plan(None, 0, None, 0) == OK
+    assert lib.adamw_plan_bytes(None, 1) == 0 and lib.adamw_plan_bytes(_array(_tensor()), -1) == 0
+    assert lib.adamw_plan_bytes(_array(_tensor(n=0, w=None)), 1) == 0
+    one = lib.adamw_plan_bytes(_array(_tensor(n=1)), 1)
+    arr = _array(_tensor(n=0), _tensor(n=100000), _tensor(n=1))
+    need = lib.adamw_plan_bytes(arr, 3)
+    assert need > one > 0
+    buf = np.zeros(need + 8, np.uint8)
+    p = buf.ctypes.data
+    assert lib.adamw_plan(arr, 3, p, need - 1) == EWORKSPACE
+    assert lib.adamw_plan(arr, 3, None, need) == EINVAL
+    assert lib.adamw_plan(arr, 3, p, need) == OK
+    assert not buf[need:].any()
+
+
+@pytest.mark.parametrize("bad", [dict(n=-1), dict(lr=float("nan")), dict(lr=float("inf")), dict(b1=1.0), dict(b1=-0.1),
+                                 dict(b2=1.0), dict(b2=float("nan")), dict(eps=-1.0), dict(eps=float("inf")),
+                                 dict(gs=float("nan")), dict(step=0), dict(plan=None), dict(plan=ctypes.c_void_p(8)),
+                                 dict(size=7), dict(n=10 ** 6), dict(n=0)])
+def test_adamw_step_refuses(lib, bad):
+    size = lib.adamw_plan_bytes(_array(_tensor()), 1)
+    a = dict(plan=P, size=size, n=1, lr=0.1, b1=0.9, b2=0.99, eps=1e-8, gs=1.0, step=1, dev=None)
+    a.update(bad)
+    assert lib.adamw_step(*a.values(), None) == EINVAL
+    assert lib.adamw_step(None, 0, 0, 0.1, 0.9, 0.99, 1e-8, 1.0, 1, None, None) == OK
