@@ -72,6 +72,10 @@ int check_tensors(const imbd_adamw_tensor *t, int n, size_t *bytes) {
   return IMBD_OK;
 }
 
+int run_product(int pass, int dtype, const ExpertArgs &a, hipStream_t s) {
+  return expert_wide_fits(pass, dtype, a) ? run_expert_wide(pass, a, s) : run_expert_tile(pass, dtype, a, s);
+}
+
 hipStream_t stream_of(void *s) { return reinterpret_cast<hipStream_t>(s); }
 
 }  // namespace
@@ -133,7 +137,7 @@ int expert_fwd(int dtype, int relu, int E, int d_out, int d_in, int n_rows, int 
   a.w = w; a.ldw = ldw; a.sw = sw; a.bias = bias; a.relu = relu != 0;
   a.x = x; a.ldx = ldx; a.rows = rows; a.offsets = offsets;
   a.out = y; a.ldo = ldy; a.out_dtype = y_dtype;
-  return run_expert_tile(EXPERT_FWD, dtype, a, stream_of(stream));
+  return run_product(EXPERT_FWD, dtype, a, stream_of(stream));
 }
 
 int expert_bwd(int dtype, int E, int d_out, int d_in, int n_rows, int n_x, const void *w, int64_t ldw, int64_t sw,
@@ -167,14 +171,14 @@ int expert_bwd(int dtype, int E, int d_out, int d_in, int n_rows, int n_x, const
     a.x = mask_relu ? x : nullptr;
     a.mask = mask_relu != 0;
     a.out = dx; a.ldo = lddx; a.out_dtype = dx_dtype;
-    TRY(run_expert_tile(EXPERT_DX, dtype, a, stream_of(stream)));
+    TRY(run_product(EXPERT_DX, dtype, a, stream_of(stream)));
   }
   if (!dw && !db) return IMBD_OK;
   a.mask = 0;
   a.x = x;
   a.out = dw; a.ldo = lddw; a.so = sdw; a.out_dtype = IMBD_F32;
   a.db = db;
-  return run_expert_tile(EXPERT_DW, dtype, a, stream_of(stream));
+  return run_product(EXPERT_DW, dtype, a, stream_of(stream));
 }
 
 int expert_combine(int dtype, int T, int k, int d, int n_rows, const void *ys, int64_t ldys, const int32_t *slots,
