@@ -6,19 +6,19 @@
 //
 // These products are bound by the matrix cores, and the tile is chosen for what feeds them: with 128 x 128
 // outputs a wave, a k-step of 32 costs 16 KB of LDS reads and 64 matrix instructions (1024 cycles), so the
-// four waves of a 256 x 256 tile read LDS half the time and its 160 KB hold the slabs of several k-steps.
-// One wave a SIMD: nothing but its own instruction order hides its waits, so
-//  * slabs of 32 k travel straight from memory to LDS through a ring of NS slots, NS - 1 k-steps ahead;
-//  * the fragments of k-step S + 1 are read between the products of k-step S, into a second register set;
-//  * one barrier a k-step, at which the wave's next products already have their operands in registers.
-// Every load of a slab is issued by every wave in every step (past the last slab with an empty buffer
-// descriptor, which fills zeros), so the number of loads in flight is the same everywhere and a wait is a
-// constant.
+// four waves of a 256 x 256 tile read LDS half the time. One wave a SIMD: nothing but its own instruction order
+// hides its waits, so
+//  * slabs of 64 k travel straight from memory to LDS, into two slots by turns. An operand by k-rows is loaded in
+//    halves of 32 k, each as soon as its place is free, three k-steps ahead; one with k contiguous as a whole, so
+//    that its rows are whole 128-byte lines (in halves the forward product took 10% longer; k-rows as a whole, the
+//    weight gradient took 13% longer);
+//  * the fragments of a k-step are read between the products of the one before, into a second register set;
+//  * one barrier a k-step (a slab, where both operands have k contiguous), at which the wave's next products
+//    already have their operands in registers.
 //
-// Slabs in LDS. An operand with k contiguous: rows of 64 bytes, the four 16-byte chunks XORed with 0, 2, 3, 1
-// for rows 0-3, 4-7, 8-11, 12-15 of sixteen. (A 16-byte read serves lanes 0-3, 12-15, 20-27 and 4-11, 16-19,
-// 28-31 of each half wave together; with these four, each such set covers all banks. 0, 1, 2, 3: twice the time.) By k-rows: quarters of 64 columns, 32 k-rows of 128
-// bytes, read with the LDS transpose read; its swizzle is that of the weight-gradient kernel.
+// Slabs in LDS. An operand with k contiguous: rows of 128 bytes, the 16-byte chunks XORed with row%8. By k-rows:
+// quarters of 64 columns, 64 k-rows of 128 bytes, read with the LDS transpose read; its swizzle is that of the
+// weight-gradient kernel. Both without bank conflicts.
 //
 // Ragged edges. Rows of an expert's last tile, output columns past the width and k past the end read as
 // zero: by lane (an offset past the buffer descriptor) or because the descriptor ends there. An expert's
@@ -32,7 +32,7 @@
 namespace imbd {
 namespace {
 
-constexpr int XW_KS = 32;                     // k per slab
+constexpr int XW_KS = 64;                     // k per slab
 constexpr int XW_GM = 8;                      // m tiles per launch-order group
 constexpr uint32_t XW_OOB = 0xffff0000u;      // past every buffer descriptor
 constexpr uint32_t XW_MOST = 0xfffe0000u;     // bytes that a descriptor covers at most
@@ -48,8 +48,6 @@ template <int N, typename F>
 __device__ __forceinline__ void static_for(F f) {
   static_for_seq(f, std::make_integer_sequence<int, N>{});
 }
-
-__device__ __forceinline__ int xw_swz_kc(int v) { return 2 * ((v ^ (v >> 1)) & 1) + (v >> 1); }  // 0, 2, 3, 1
 
 // One wave writes 64 x 16 bytes to LDS at lds_base + 16*lane, from byte offsets voff + IMM of the buffer. (The
 // instruction's own offset counts on both sides, so it is taken off the LDS base.)
@@ -76,53 +74,80 @@ __device__ __forceinline__ void mfma_v(f32x4 &acc, const bf16x8 &a, const bf16x8
 // Wait states between the last product and the first read of its result (the compiler does not see them).
 __device__ __forceinline__ void mfma_drain() { asm volatile("s_nop 15\n\ts_nop 15" : : : "memory"); }
 
-// A buffer descriptor that moves by `step` bytes a slab: `most` bytes on every slab, `last` on the one that
-// holds the end of k, none past it.
+// Which of nl loads, spread over the first `span` products, goes with product p: load q with product q*span/nl,
+// rounded down to an even one. nl: none.
+constexpr int xw_load_at(int p, int nl, int span) {
+  for (int q = 0; q < nl; ++q)
+    if (q * span / nl / 2 * 2 == p) return q;
+  return nl;
+}
+
+// A product and, in the wait state that a write of m0 asks for, behind it a load to LDS (as dma16_at).
+template <int IMM>
+__device__ __forceinline__ void mfma_dma16(f32x4 &acc, const bf16x8 &a, const bf16x8 &b, const i32x4 &rsrc, uint32_t voff,
+                                           uint32_t lds_base) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0\n\tbuffer_load_dwordx4 %3, %4, 0 offen offset:%6 lds"
+               : "+a"(acc)
+               : "v"(a), "v"(b), "v"(voff), "s"(rsrc), "{m0}"(lds_base - IMM), "n"(IMM)
+               : "memory");
+}
+// Waits for this wave's LDS reads and, BARRIER, for all but VM of its loads and for every wave. (The builtins, so
+// that the compiler knows that the reads have landed and adds no waits of its own.)
+template <bool BARRIER, int VM = 0>
+__device__ __forceinline__ void step_wait() {
+  static_assert(VM < 64, "");
+  asm volatile("" : : : "memory");
+  if constexpr (BARRIER) {
+    __builtin_amdgcn_s_waitcnt((VM & 15) | ((VM >> 4) << 14) | 0x70);
+    __builtin_amdgcn_s_barrier();
+  } else {
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+  }
+  asm volatile("" : : : "memory");
+}
+
+// A buffer descriptor that moves `step` bytes a slab: `most` bytes on every slab, `last` on the one that holds the
+// end of k, none past it.
 struct Window {
-  uint64_t base;
+  i32x4 r;
   int64_t step;
-  uint32_t most, last;
-  __device__ __forceinline__ i32x4 next(bool live, bool ends) {
-    const i32x4 r = buf_rsrc(reinterpret_cast<const void *>(base), live ? (ends ? last : most) : 0u);
-    base += (uint64_t)step;
-    return r;
+  uint32_t last;
+  __device__ __forceinline__ Window(const void *p, int64_t step_, uint32_t most, uint32_t last_)
+      : r(buf_rsrc(p, most)), step(step_), last(last_) {}
+  __device__ __forceinline__ void advance() {  // (addresses have 48 bits: no carry reaches the stride field)
+    const uint64_t b = (((uint64_t)(uint32_t)r[1] << 32) | (uint32_t)r[0]) + (uint64_t)step;
+    r[0] = (int)(uint32_t)b;
+    r[1] = (int)(uint32_t)(b >> 32);
   }
 };
 
-// One operand's slab: R rows (or columns) of the tile, loaded by four waves. KC: k contiguous (R rows of 64
-// bytes); else by k-rows (32 k-rows of R columns).
-template <int R, bool KC>
-struct Slab {
-  static constexpr int BYTES = R * 64;
-  static constexpr int PER = R / 64;  // loads a wave
-  uint32_t voff[KC ? PER : 1];        // k-rows: one offset, the quarters 128 bytes apart
-};
-
-template <int PASS, int BM, int BN, int NS>
+template <int PASS, int BM, int BN>
 struct Shape {
   static constexpr bool A_KC = PASS == EXPERT_FWD, B_KC = PASS != EXPERT_DW;
   static constexpr int FM = BM / 32, FN = BN / 32;  // 16-wide blocks of a wave (2 x 2 waves)
-  static constexpr int SLAB = (BM + BN) * 64;
-  static constexpr int RING = NS * SLAB;
-  static constexpr int LOADS = BM / 64 + BN / 64;   // a wave, a slab
+  static constexpr int SLAB = (BM + BN) * 128;
+  static constexpr int PA = BM / 32, PB = BN / 32;  // loads a wave, a slab
+  // ... in k-step h: half of a k-row operand's in each, a k-contiguous operand's in the second
+  static constexpr int la(int h) { return A_KC ? (h ? PA : 0) : PA / 2; }
+  static constexpr int lb(int h) { return B_KC ? (h ? PB : 0) : PB / 2; }
+  static constexpr int loads(int h) { return la(h) + lb(h); }
 };
 
-template <int PASS, int BM, int BN, int NS, bool GATHER>
+template <int PASS, int BM, int BN, bool GATHER>
 constexpr int xw_lds_bytes() {
-  // the ring; Delta_W with gathered x: the row indices of 2*NS slabs, 256 bytes a wave each
-  constexpr int ring = Shape<PASS, BM, BN, NS>::RING + (PASS == EXPERT_DW && GATHER ? 2 * NS * 1024 : 0);
+  // two slots; Delta_W with gathered x: the row indices of eight half slabs, 256 bytes a wave each
+  constexpr int ring = 2 * Shape<PASS, BM, BN>::SLAB + (PASS == EXPERT_DW && GATHER ? 8 * 1024 : 0);
   constexpr int stage = 4 * 16 * (BM / 2 * 4 + 16);  // the epilogue: 16 rows of each wave
   return ring > stage ? ring : stage;
 }
 
-template <int PASS, int BM, int BN, int NS, bool GATHER, int WGS>
+template <int PASS, int BM, int BN, bool GATHER, int WGS>
 __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int tiles_m, int tiles_n) {
-  using Sh = Shape<PASS, BM, BN, NS>;
+  using Sh = Shape<PASS, BM, BN>;
   constexpr bool A_KC = Sh::A_KC, B_KC = Sh::B_KC;
   constexpr int FM = Sh::FM, FN = Sh::FN;
   constexpr bool GATHER_W = PASS == EXPERT_DW && GATHER;  // x by k-rows, each from its own row
-  constexpr int LOADS = Sh::LOADS + (GATHER_W ? 1 : 0);
-  __shared__ __attribute__((aligned(1024))) char smem[xw_lds_bytes<PASS, BM, BN, NS, GATHER>()];
+  __shared__ __attribute__((aligned(1024))) char smem[xw_lds_bytes<PASS, BM, BN, GATHER>()];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
@@ -155,124 +180,153 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     if (!find_row_tile<BN>(a, tn, &e, &n0, &n_end)) return;
     K = PASS == EXPERT_FWD ? a.d_in : a.d_out;
   }
-  const int nsl = (K + XW_KS - 1) / XW_KS;
+  const int nsl = (K + XW_KS - 1) / XW_KS, nhs = (K + 31) / 32;  // slabs, half slabs
   const uint16_t *w = reinterpret_cast<const uint16_t *>(a.w) + (int64_t)e * a.sw;
   const uint16_t *x = reinterpret_cast<const uint16_t *>(a.x);
   const uint16_t *dy = reinterpret_cast<const uint16_t *>(a.dy);
 
   // ---- sources: a window on each operand and every lane's offsets in it
-  Slab<BM, A_KC> sa;
-  Slab<BN, B_KC> sb;
-  Window wa, wb;
-  const int kc = 8 * ((lane & 3) ^ xw_swz_kc(lane >> 4));            // k-contiguous: this lane's first k in a slab
-  const int kr = 8 * wave + (lane >> 3);                           // k-rows: this lane's row of a slab
+  // (k contiguous: a piece is 8 rows; k-rows: 8 k-rows of one quarter, a wave's rows 8*wave .. +7 of a half slab)
+  uint32_t va[A_KC ? Sh::PA : 1], vb[B_KC ? Sh::PB : 1];
+  const int kc = 8 * ((lane & 7) ^ (lane >> 3));                   // k contiguous: this lane's first k in a slab
+  const int kr = 8 * wave + (lane >> 3);                           // k-rows: this lane's row of a half slab
   const uint32_t kcol = (uint32_t)(16 * ((lane & 7) ^ xw_swz_tr(kr)));  // ... and byte column of a quarter
-  const int k_last = K - (nsl - 1) * XW_KS;                        // k of the last slab
-  // rows of k: 32 of them (k_last in the last slab) of `cols` columns from the window's base on
+  const int k_last = K - (nsl - 1) * XW_KS, h_last = K - (nhs - 1) * 32;  // k of the last slab, half slab
+  // rows of k: 32 of them (h_last in the last half slab) of `cols` columns from the window's base on
   auto k_rows = [&](const uint16_t *p, int64_t ld, int cols) {
-    return Window{(uint64_t)(uintptr_t)p, XW_KS * ld * 2, (uint32_t)(((XW_KS - 1) * ld + cols) * 2),
-                  (uint32_t)(((k_last - 1) * ld + cols) * 2)};
+    return Window(p, 32 * ld * 2, (uint32_t)(((h_last < K ? 31 : h_last - 1) * ld + cols) * 2),
+                  (uint32_t)(((h_last - 1) * ld + cols) * 2));
   };
   // k contiguous: `rows` rows (what lies past k in the last slab is masked by lane)
   auto k_cols = [&](const uint16_t *p, int64_t ld, int64_t rows) {
     const uint32_t n = rows > 0 ? (uint32_t)(((rows - 1) * ld + min(K, XW_KS)) * 2) : 0u;
-    return Window{(uint64_t)(uintptr_t)p, XW_KS * 2, n, rows > 0 ? (uint32_t)(((rows - 1) * ld + k_last) * 2) : 0u};
+    return Window(p, XW_KS * 2, n, rows > 0 ? (uint32_t)(((rows - 1) * ld + k_last) * 2) : 0u);
   };
-  if constexpr (A_KC) {
-    wa = k_cols(w + (int64_t)m0 * a.ldw, a.ldw, min(BM, M - m0));
-#pragma unroll
-    for (int q = 0; q < BM / 64; ++q) {
-      const int r = 16 * (BM / 64 * wave + q) + (lane >> 2);
-      sa.voff[q] = m0 + r < M ? (uint32_t)(((int64_t)r * a.ldw + kc) * 2) : XW_OOB;
+  Window wa = [&] {
+    if constexpr (A_KC) {
+      return k_cols(w + (int64_t)m0 * a.ldw, a.ldw, min(BM, M - m0));
+    } else if constexpr (PASS == EXPERT_DX) {
+      return k_rows(w + m0, a.ldw, M - m0);
+    } else if constexpr (!GATHER) {
+      return k_rows(x + (int64_t)r0 * a.ldx + m0, a.ldx, M - m0);
+    } else {  // any row of x: the k-rows that do not exist are masked by lane
+      const uint32_t n = a.n_x > 0 ? (uint32_t)(((int64_t)(a.n_x - 1) * a.ldx + M - m0) * 2) : 0u;
+      return Window(x + m0, 0, n, n);
     }
-  } else if constexpr (PASS == EXPERT_DX) {
-    wa = k_rows(w + m0, a.ldw, M - m0);
-    sa.voff[0] = (uint32_t)((int64_t)kr * a.ldw * 2) + kcol;
-  } else if constexpr (!GATHER) {
-    wa = k_rows(x + (int64_t)r0 * a.ldx + m0, a.ldx, M - m0);
-    sa.voff[0] = (uint32_t)((int64_t)kr * a.ldx * 2) + kcol;
-  } else {
-    // (any row of x: the rows that do not exist are masked by lane)
-    const uint32_t n = a.n_x > 0 ? (uint32_t)(((int64_t)(a.n_x - 1) * a.ldx + M - m0) * 2) : 0u;
-    wa = Window{(uint64_t)(uintptr_t)(x + m0), 0, n, n};
-    sa.voff[0] = XW_OOB;
-  }
-  if constexpr (B_KC) {
-    constexpr bool G = PASS == EXPERT_FWD && GATHER;
-    const int64_t ld = PASS == EXPERT_FWD ? a.ldx : a.lddy;
-    const uint16_t *src = PASS == EXPERT_FWD ? x : dy;
-    wb = k_cols(G ? src : src + (int64_t)n0 * ld, ld, G ? a.n_x : min(BN, n_end - n0));
+  }();
+  if constexpr (A_KC) {
 #pragma unroll
-    for (int q = 0; q < BN / 64; ++q) {
-      const int r = 16 * (BN / 64 * wave + q) + (lane >> 2);
+    for (int q = 0; q < Sh::PA; ++q) {
+      const int r = 8 * (Sh::PA * wave + q) + (lane >> 3);
+      va[q] = m0 + r < M ? (uint32_t)(((int64_t)r * a.ldw + kc) * 2) : XW_OOB;
+    }
+  } else {
+    va[0] = GATHER_W ? XW_OOB : (uint32_t)((int64_t)kr * (PASS == EXPERT_DX ? a.ldw : a.ldx) * 2) + kcol;
+  }
+  constexpr bool GATHER_X = PASS == EXPERT_FWD && GATHER;  // x by rows, each from its own row
+  const int64_t ldb = PASS == EXPERT_FWD ? a.ldx : a.lddy;
+  Window wb = [&] {
+    if constexpr (!B_KC) return k_rows(dy + (int64_t)r0 * a.lddy + n0, a.lddy, n_end - n0);
+    else if constexpr (GATHER_X) return k_cols(x, ldb, a.n_x);
+    else return k_cols((PASS == EXPERT_FWD ? x : dy) + (int64_t)n0 * ldb, ldb, min(BN, n_end - n0));
+  }();
+  if constexpr (B_KC) {
+#pragma unroll
+    for (int q = 0; q < Sh::PB; ++q) {
+      const int r = 8 * (Sh::PB * wave + q) + (lane >> 3);
       bool ok = n0 + r < n_end;
       int row = r;
-      if constexpr (G) {
+      if constexpr (GATHER_X) {
         row = ok ? a.rows[n0 + r] : -1;
         ok = row >= 0 && row < a.n_x;
       }
-      sb.voff[q] = ok ? (uint32_t)row * (uint32_t)(ld * 2) + (uint32_t)(kc * 2) : XW_OOB;
+      vb[q] = ok ? (uint32_t)row * (uint32_t)(ldb * 2) + (uint32_t)(kc * 2) : XW_OOB;
     }
   } else {
-    wb = k_rows(dy + (int64_t)r0 * a.lddy + n0, a.lddy, n_end - n0);
-    sb.voff[0] = (uint32_t)((int64_t)kr * a.lddy * 2) + kcol;
+    vb[0] = (uint32_t)((int64_t)kr * a.lddy * 2) + kcol;
   }
 
-  // the row indices of gathered k-rows: lane l's of slab X at idx0 + (X % 2NS)*1024 + 4l
-  const uint32_t idx0 = lds0 + (uint32_t)(Sh::RING + wave * 256);
+  // the row indices of gathered k-rows: lane l's of half slab Y at idx0 + (Y % 8)*1024 + 4l
+  const uint32_t idx0 = lds0 + (uint32_t)(2 * Sh::SLAB + wave * 256 + 4 * lane);
   const i32x4 ri = GATHER_W ? buf_rsrc(a.rows + r0, (uint32_t)K * 4u) : i32x4{0, 0, 0, 0};
-  auto load_index = [&](int X) {
+  auto load_index = [&](int Y) {
     if constexpr (GATHER_W)
-      dma4(ri, (uint32_t)(X * XW_KS + kr) * 4u, idx0 + (uint32_t)((X % (2 * NS)) * 1024));
+      dma4(ri, (uint32_t)(Y * 32 + kr) * 4u, lds0 + (uint32_t)(2 * Sh::SLAB + wave * 256 + (Y & 7) * 1024));
   };
-  auto index_of = [&](int X) {  // (its indices have landed)
-    return *(const __attribute__((address_space(3))) int *)(uintptr_t)(idx0 + (uint32_t)((X % (2 * NS)) * 1024 + 4 * lane));
+  auto index_of = [&](int Y) {  // (its indices have landed)
+    return *(const __attribute__((address_space(3))) int *)(uintptr_t)(idx0 + (uint32_t)((Y & 7) * 1024));
   };
-  auto gather = [&](int X, int row) {  // the offsets of slab X
-    const bool ok = X * XW_KS + kr < K && row >= 0 && row < a.n_x;
-    sa.voff[0] = ok ? (uint32_t)row * (uint32_t)(a.ldx * 2) + kcol : XW_OOB;
+  auto gather = [&](int Y, int row) {  // the offsets of half slab Y
+    const bool ok = Y * 32 + kr < K && row >= 0 && row < a.n_x;
+    va[0] = ok ? (uint32_t)row * (uint32_t)(a.ldx * 2) + kcol : XW_OOB;
   };
 
-  // ---- loads of slab X, in LOADS pieces (slabs in order: the windows move on)
-  i32x4 ra, rb;
-  uint32_t slot_w = 0;
-  bool past = false;  // this lane's k lies past the end (k contiguous)
-  auto open_a = [&](int X) {
-    ra = wa.next(X < nsl, X == nsl - 1);
-    slot_w = lds0 + (uint32_t)((X % NS) * Sh::SLAB);
+  // ---- loads, in the order of half slabs Y = 2 X + h (the windows move on); k-contiguous operands with h = 1
+  auto ends = [&](int Y, auto htag) {  // before the loads of Y: the last ones and those past them
+    constexpr int h = decltype(htag)::value;
+    if constexpr ((!A_KC && !GATHER_W) || !B_KC) {
+      if (Y >= nhs - 1) {
+        if constexpr (!A_KC && !GATHER_W) wa.r[2] = Y == nhs - 1 ? (int)wa.last : 0;
+        if constexpr (!B_KC) wb.r[2] = Y == nhs - 1 ? (int)wb.last : 0;
+      }
+    }
+    if constexpr ((A_KC || B_KC) && h == 1) {
+      const int X = Y >> 1;
+      if (X >= nsl - 1) {
+        if constexpr (A_KC) wa.r[2] = X == nsl - 1 ? (int)wa.last : 0;
+        if constexpr (B_KC) wb.r[2] = X == nsl - 1 ? (int)wb.last : 0;
+        const bool past = kc >= k_last;  // this lane's k lies past the end
+        if constexpr (A_KC)
+#pragma unroll
+          for (int q = 0; q < Sh::PA; ++q) va[q] = past ? XW_OOB : va[q];
+        if constexpr (B_KC)
+#pragma unroll
+          for (int q = 0; q < Sh::PB; ++q) vb[q] = past ? XW_OOB : vb[q];
+      }
+    }
   };
-  auto open_b = [&](int X) {
-    rb = wb.next(X < nsl, X == nsl - 1);
-    if constexpr (A_KC || B_KC) past = X * XW_KS + kc >= K;
+  auto advance = [&](auto htag) {
+    constexpr int h = decltype(htag)::value;
+    if constexpr ((A_KC && h == 1) || (!A_KC && !GATHER_W)) wa.advance();
+    if constexpr (h == 1 || !B_KC) wb.advance();
   };
-  auto piece = [&](auto qtag) {
-    constexpr int q = decltype(qtag)::value;
-    if constexpr (q < BM / 64) {
-      if constexpr (A_KC) dma16_at<0>(ra, past ? XW_OOB : sa.voff[q], slot_w + (uint32_t)((BM / 64 * wave + q) * 1024));
-      else dma16_at<128 * q>(ra, sa.voff[0], slot_w + (uint32_t)(q * 4096 + wave * 1024));
-    } else if constexpr (q < Sh::LOADS) {
-      constexpr int p = q - BM / 64;
-      const uint32_t to = slot_w + (uint32_t)(BM * 64);
-      if constexpr (B_KC) dma16_at<0>(rb, past ? XW_OOB : sb.voff[p], to + (uint32_t)((BN / 64 * wave + p) * 1024));
-      else dma16_at<128 * p>(rb, sb.voff[0], to + (uint32_t)(p * 4096 + wave * 1024));
+  // piece q of the loads of k-step h into slot t, by f(descriptor, offset, LDS address, instruction's offset)
+  auto piece = [&](auto ttag, auto htag, auto qtag, auto f) {
+    constexpr int t = decltype(ttag)::value, h = decltype(htag)::value, q = decltype(qtag)::value;
+    constexpr uint32_t slot = (uint32_t)(t * Sh::SLAB);
+    if constexpr (q < Sh::la(h)) {
+      if constexpr (A_KC) f(wa.r, va[q], lds0 + (uint32_t)(wave * Sh::PA * 1024) + slot + q * 1024, std::integral_constant<int, 0>{});
+      else f(wa.r, va[0], lds0 + (uint32_t)(wave * 1024) + slot + q * 8192 + h * 4096, std::integral_constant<int, 128 * q>{});
+    } else {
+      constexpr int p = q - Sh::la(h);
+      constexpr uint32_t to = slot + (uint32_t)(BM * 128);
+      if constexpr (B_KC) f(wb.r, vb[p], lds0 + (uint32_t)(wave * Sh::PB * 1024) + to + p * 1024, std::integral_constant<int, 0>{});
+      else f(wb.r, vb[0], lds0 + (uint32_t)(wave * 1024) + to + p * 8192 + h * 4096, std::integral_constant<int, 128 * p>{});
     }
   };
 
   // ---- fragments
   const int fi = lane & 15, kg = lane >> 4, wm = wave & 1, wn = wave >> 1;
   const int tr = 8 * kg + (fi >> 2);
-  uint32_t fa[A_KC ? 1 : 4], fb[B_KC ? 1 : 4];
-  {
-    const uint32_t kcl = (uint32_t)(fi * 64 + ((kg ^ xw_swz_kc(fi >> 2)) * 16));
-    if constexpr (A_KC) fa[0] = lds0 + (uint32_t)(wm * FM * 1024) + kcl;
-    if constexpr (B_KC) fb[0] = lds0 + (uint32_t)(BM * 64 + wn * FN * 1024) + kcl;
+  // addresses of k-step 0 (k contiguous: and of k-step 1) of slot 0, then those of slot 1: the rest of a read's
+  // address is a constant of the instruction
+  constexpr int NA = A_KC ? 2 : 4, NB = B_KC ? 2 : 4;
+  uint32_t fa[2][NA], fb[2][NB];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t c = (uint32_t)(((2 * j + ((fi >> 1) & 1)) ^ xw_swz_tr(tr)) * 16 + tr * 128 + 8 * (fi & 1));
-      // (a wave's blocks start on a quarter or, 32-wide waves, in the middle of one)
-      if constexpr (!A_KC) fa[j] = lds0 + (uint32_t)(wm * FM / 4 * 4096) + c;
-      if constexpr (!B_KC) fb[j] = lds0 + (uint32_t)(BM * 64 + wn * FN / 4 * 4096) + c;
+      const uint32_t slot = lds0 + (uint32_t)(t * Sh::SLAB);
+      const uint32_t kcl = (uint32_t)(fi * 128 + (((4 * j + kg) ^ (fi & 7)) * 16));
+      const uint32_t trr = (uint32_t)(((2 * j + ((fi >> 1) & 1)) ^ xw_swz_tr(tr)) * 16 + tr * 128 + 8 * (fi & 1));
+      if (j < NA) fa[t][j] = slot + (A_KC ? (uint32_t)(wm * FM * 2048) + kcl : (uint32_t)(wm * FM / 4 * 8192) + trr);
+      if (j < NB)
+        fb[t][j] = slot + (uint32_t)(BM * 128) + (B_KC ? (uint32_t)(wn * FN * 2048) + kcl : (uint32_t)(wn * FN / 4 * 8192) + trr);
     }
+#pragma unroll
+    for (int j = 0; j < NA; ++j) asm volatile("" : "+v"(fa[t][j]));
+#pragma unroll
+    for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(fb[t][j]));
   }
   static_assert(FM % 4 == 0 && FN % 4 == 0, "k-row fragments come in whole quarters");
   auto lds16 = [](uint32_t p) {
@@ -284,13 +338,14 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(q + 4 * 128 / 8);
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  auto read_a = [&](uint32_t slot, int i) {
-    if constexpr (A_KC) return lds16(fa[0] + slot + (uint32_t)(i * 1024));
-    else return lds_tr(fa[i & 3] + slot + (uint32_t)((i >> 2) * 4096));
+  // block i of k-step h of the slab in slot t
+  auto read_a = [&](int t, int h, int i) {
+    if constexpr (A_KC) return lds16(fa[t][h] + (uint32_t)(i * 2048));
+    else return lds_tr(fa[t][i & 3] + (uint32_t)((i >> 2) * 8192 + h * 4096));
   };
-  auto read_b = [&](uint32_t slot, int j) {
-    if constexpr (B_KC) return lds16(fb[0] + slot + (uint32_t)(j * 1024));
-    else return lds_tr(fb[j & 3] + slot + (uint32_t)((j >> 2) * 4096));
+  auto read_b = [&](int t, int h, int j) {
+    if constexpr (B_KC) return lds16(fb[t][h] + (uint32_t)(j * 2048));
+    else return lds_tr(fb[t][j & 3] + (uint32_t)((j >> 2) * 8192 + h * 4096));
   };
 
   f32x4 acc[FM][FN], accd[PASS == EXPERT_DW ? FN : 1];
@@ -305,82 +360,104 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     for (int j = 0; j < FN; ++j) accd[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
 
-  // ---- the first NS slabs (and the indices of 2 NS)
+  // ---- the first two slabs (and the indices of eight half slabs)
+  const std::integral_constant<int, 0> c0{};
+  const std::integral_constant<int, 1> c1{};
   if constexpr (GATHER_W) {
 #pragma unroll
-    for (int X = 0; X < 2 * NS; ++X) load_index(X);
+    for (int Y = 0; Y < 8; ++Y) load_index(Y);
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
   }
-  // (a slab's loads end with the index load of the slab NS after it; the first NS slabs repeat one instead,
-  // which keeps their number)
-#pragma unroll
-  for (int X = 0; X < NS; ++X) {
-    if constexpr (GATHER_W) gather(X, index_of(X));
-    open_a(X);
-    open_b(X);
-    static_for<Sh::LOADS>(piece);
-    load_index(X);
-  }
+  auto first = [&](auto ttag, auto htag) {
+    constexpr int t = decltype(ttag)::value, h = decltype(htag)::value;
+    if constexpr (GATHER_W) gather(2 * t + h, index_of(2 * t + h));
+    ends(2 * t + h, htag);
+    static_for<Sh::loads(h)>([&](auto q) {
+      piece(ttag, htag, q,
+            [&](const i32x4 &r, uint32_t voff, uint32_t to, auto imm) { dma16_at<decltype(imm)::value>(r, voff, to); });
+    });
+    advance(htag);
+  };
+  first(c0, c0);
+  first(c0, c1);
+  first(c1, c0);
+  load_index(6);  // (again: every k-step's loads end with one)
+  first(c1, c1);
+  load_index(7);
+  // loads that may be under way when k-step h begins. Its fragment reads take a half slab loaded three k-steps ago,
+  // for h = 1 a k-contiguous operand's slab loaded two ago.
+  constexpr int IDX = GATHER_W ? 1 : 0;
+  constexpr int VM0 = Sh::loads(0) + Sh::loads(1) + 2 * IDX, VM1 = A_KC || B_KC ? Sh::loads(0) : VM0;
+  constexpr bool BOTH_KC = A_KC && B_KC;
 
   bf16x8 av[2][FM], bv[2][FN];
-  vm_barrier<LOADS * (NS - 1)>();  // slab 0
+  step_wait<true, VM0>();  // slab 0
 #pragma unroll
-  for (int i = 0; i < FM; ++i) av[0][i] = read_a(0, i);
+  for (int i = 0; i < FM; ++i) av[0][i] = read_a(0, 0, i);
 #pragma unroll
-  for (int j = 0; j < FN; ++j) bv[0][j] = read_b(0, j);
+  for (int j = 0; j < FN; ++j) bv[0][j] = read_b(0, 0, j);
+  if constexpr (GATHER_W) gather(4, index_of(4));
+  ends(4, c0);
 
-  auto step = [&](int S, auto ctag) {
-    constexpr int c = decltype(ctag)::value;
-    // slab S + 1 has landed everywhere, and every wave has slab S in registers: its slot is free
-    vm_barrier<LOADS * (NS - 2)>();
-    const uint32_t slot = (uint32_t)(((S + 1) % NS) * Sh::SLAB);
-    const int X = S + NS;
+  // k-step h of slab S, which lies in slot t = S % 2. Between its products, one by one, what else there is to do, so
+  // that it fits in their shadow (a wave issues an instruction every four cycles, a product takes sixteen; all the
+  // scalar work of a slab in one place left the matrix cores idle for 15% of the time): the fragments of the next
+  // k-step, the loads of slab S + 2 into what every wave has read, and what the next loads need.
+  auto step = [&](int S, auto ttag, auto htag) {
+    constexpr int t = decltype(ttag)::value, h = decltype(htag)::value;
+    if constexpr (h == 0) step_wait<!BOTH_KC, VM0>();
+    else step_wait<true, VM1>();
+    const int Y = 2 * S + h;
     int row = 0;
-    // The step's FM * FN products in pairs, and before each pair what fits its 32 cycles: the reads of k-step
-    // S + 1 in the first half, then the windows and the loads of slab S + NS. (All the scalar work of a slab in
-    // one place left the matrix cores idle for 15% of the step.)
-    constexpr int NP = FM * FN / 2, RP = NP / 2, NR = FM + FN, LP = NP - RP - 4;
-    static_for<NP>([&](auto ptag) {
+    constexpr int NM = FM * FN, NR = FM + FN, NL = Sh::loads(h), SPAN = NM < 3 * NL ? NM : 3 * NL;
+    static_assert(NM >= 2 * NR + 8 && SPAN >= 2 * NL, "");
+    static_for<NM>([&](auto ptag) {
       constexpr int p = decltype(ptag)::value;
-      if constexpr (p < RP) {
-        if constexpr (GATHER_W && p == 0) row = index_of(X);
-#pragma unroll
-        for (int r = p * NR / RP; r < (p + 1) * NR / RP; ++r) {
-          // (a and b by turns, then what is left of the longer)
-          constexpr int both = 2 * (FM < FN ? FM : FN);
-          const bool is_a = r < both ? r % 2 == 0 : FM > FN;
-          const int at = r < both ? r / 2 : r - both / 2;
-          if (is_a) av[c ^ 1][at < FM ? at : 0] = read_a(slot, at);
-          else bv[c ^ 1][at < FN ? at : 0] = read_b(slot, at);
-        }
-      } else if constexpr (p == RP) {
-        open_a(X);
-      } else if constexpr (p == RP + 2) {
-        open_b(X);
-        if constexpr (GATHER_W) gather(X, row);
-      } else if constexpr (p >= RP + 4) {
-        constexpr int l = p - RP - 4, lo = l * Sh::LOADS / LP, hi = (l + 1) * Sh::LOADS / LP;
-        static_for<hi - lo>([&](auto q) { piece(std::integral_constant<int, lo + decltype(q)::value>{}); });
-        if constexpr (p == NP - 1) load_index(X + NS);
+      f32x4 &d = acc[p / FN][p % FN];
+      const bf16x8 &ma = av[h][p / FN], &mb = bv[h][p % FN];
+      // read r before every odd product: a and b by turns, then what is left of the longer
+      constexpr int r = p % 2 == 1 ? p / 2 : NR;
+      constexpr int both = 2 * (FM < FN ? FM : FN);
+      constexpr bool is_a = r < both ? r % 2 == 0 : FM > FN;
+      constexpr int at = r < both ? r / 2 : r - both / 2;
+      if constexpr (r < NR) {
+        if constexpr (is_a) av[h ^ 1][at] = read_a(h == 0 ? t : t ^ 1, h ^ 1, at);
+        else bv[h ^ 1][at] = read_b(h == 0 ? t : t ^ 1, h ^ 1, at);
       }
-      mfma(acc[2 * p / FN][2 * p % FN], av[c][2 * p / FN], bv[c][2 * p % FN]);
-      mfma(acc[2 * p / FN][2 * p % FN + 1], av[c][2 * p / FN], bv[c][2 * p % FN + 1]);
+      // load q with an even product
+      constexpr int q = xw_load_at(p, NL, SPAN);
+      if constexpr (q < NL) {
+        piece(ttag, htag, std::integral_constant<int, q>{}, [&](const i32x4 &r, uint32_t voff, uint32_t to, auto imm) {
+          mfma_dma16<decltype(imm)::value>(d, ma, mb, r, voff, to);
+        });
+      } else {
+        mfma(d, ma, mb);
+      }
+      if constexpr (p == NM - 14) {
+        advance(htag);
+        if constexpr (GATHER_W) {
+          load_index(Y + 8);  // (landed three k-steps on, read one after that)
+          row = index_of(Y + 5);
+        }
+      }
+      if constexpr (GATHER_W && p == NM - 6) gather(Y + 5, row);
+      if constexpr (p == NM - 3) ends(Y + 5, std::integral_constant<int, h ^ 1>{});
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (PASS == EXPERT_DW) {
       if (do_db) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-          mfma_v(accd[j], ones, bv[c][j]);
+        for (int j = 0; j < FN; ++j) mfma_v(accd[j], ones, bv[h][j]);
       }
     }
   };
-  int S = 0;
-  for (; S + 2 <= nsl; S += 2) {
-    step(S, std::integral_constant<int, 0>{});
-    step(S + 1, std::integral_constant<int, 1>{});
+  // (slabs in pairs, so that slots and register sets are constants: one past the last is zeros)
+  for (int S = 0; S < nsl; S += 2) {
+    step(S, c0, c0);
+    step(S, c0, c1);
+    step(S + 1, c1, c0);
+    step(S + 1, c1, c1);
   }
-  if (S < nsl) step(S, std::integral_constant<int, 0>{});
   vm_barrier<0>();  // LDS is free: nothing is in flight and every wave is done reading
   mfma_drain();
 #pragma unroll
@@ -503,7 +580,7 @@ bool expert_wide_fits(int pass, int dtype, const ExpertArgs &a) {
   return a.n_rows < (1 << 29);  // byte offsets into rows
 }
 
-template <int PASS, int BM, int BN, int NS, int WGS>
+template <int PASS, int BM, int BN, int WGS>
 static int launch(const ExpertArgs &a, hipStream_t s) {
   const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in;
   const int64_t tm = PASS == EXPERT_DW && !a.out ? 1 : (M + BM - 1) / BM;
@@ -517,19 +594,19 @@ static int launch(const ExpertArgs &a, hipStream_t s) {
   {
     LaunchTimer t(IMBD_K_EXPERT_FWD + PASS, 0, s);
     if (a.rows && PASS != EXPERT_DX)
-      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, NS, true, WGS>), grid, dim3(256), 0, s, a, (int)tm,
+      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, true, WGS>), grid, dim3(256), 0, s, a, (int)tm,
                          (int)(PASS == EXPERT_DW ? tn : rows));
     else
-      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, NS, false, WGS>), grid, dim3(256), 0, s, a, (int)tm,
+      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, false, WGS>), grid, dim3(256), 0, s, a, (int)tm,
                          (int)(PASS == EXPERT_DW ? tn : rows));
   }
   return check_launch("expert_wide");
 }
 
 int run_expert_wide(int pass, const ExpertArgs &a, hipStream_t s) {
-  if (pass == EXPERT_FWD) return launch<EXPERT_FWD, 256, 256, 4, 1>(a, s);
-  if (pass == EXPERT_DX) return launch<EXPERT_DX, 256, 256, 4, 1>(a, s);
-  return launch<EXPERT_DW, 256, 256, 4, 1>(a, s);
+  if (pass == EXPERT_FWD) return launch<EXPERT_FWD, 256, 256, 1>(a, s);
+  if (pass == EXPERT_DX) return launch<EXPERT_DX, 256, 256, 1>(a, s);
+  return launch<EXPERT_DW, 256, 256, 1>(a, s);
 }
 
 }  // namespace imbd
