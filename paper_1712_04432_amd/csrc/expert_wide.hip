@@ -13,7 +13,8 @@
 //    that its rows are whole 128-byte lines (in halves the forward product took 10% longer; k-rows as a whole, the
 //    weight gradient took 13% longer);
 //  * the fragments of a k-step are read between the products of the one before, into a second register set;
-//  * one barrier a k-step (a slab, where both operands have k contiguous), at which the wave's next products
+//  * one barrier a k-step (a slab, where both operands have k contiguous: one of them then has three slots, so that
+//    their loads take turns; all in one k-step, the loads themselves waited for their place), at which the wave's next products
 //    already have their operands in registers.
 //
 // Slabs in LDS. An operand with k contiguous: rows of 128 bytes, the 16-byte chunks XORed with row%8. By k-rows:
@@ -125,18 +126,22 @@ template <int PASS, int BM, int BN>
 struct Shape {
   static constexpr bool A_KC = PASS == EXPERT_FWD, B_KC = PASS != EXPERT_DW;
   static constexpr int FM = BM / 32, FN = BN / 32;  // 16-wide blocks of a wave (2 x 2 waves)
-  static constexpr int SLAB = (BM + BN) * 128;
+  // B in three slots where both operands have k contiguous: its loads then go with the k-steps that A's do not take
+  static constexpr bool TRI = A_KC && B_KC;
+  static constexpr int SA = BM * 128, SB = BN * 128;  // a slot of each
+  static constexpr int RING = 2 * SA + (TRI ? 3 : 2) * SB;
   static constexpr int PA = BM / 32, PB = BN / 32;  // loads a wave, a slab
-  // ... in k-step h: half of a k-row operand's in each, a k-contiguous operand's in the second
+  // ... in k-step h: half of a k-row operand's in each, a k-contiguous operand's in the second (TRI: B's in the first)
+  static constexpr int HB = TRI ? 0 : 1;
   static constexpr int la(int h) { return A_KC ? (h ? PA : 0) : PA / 2; }
-  static constexpr int lb(int h) { return B_KC ? (h ? PB : 0) : PB / 2; }
+  static constexpr int lb(int h) { return B_KC ? (h == HB ? PB : 0) : PB / 2; }
   static constexpr int loads(int h) { return la(h) + lb(h); }
 };
 
 template <int PASS, int BM, int BN, bool GATHER>
 constexpr int xw_lds_bytes() {
-  // two slots; Delta_W with gathered x: the row indices of eight half slabs, 256 bytes a wave each
-  constexpr int ring = 2 * Shape<PASS, BM, BN>::SLAB + (PASS == EXPERT_DW && GATHER ? 8 * 1024 : 0);
+  // the slots; Delta_W with gathered x: the row indices of eight half slabs, 256 bytes a wave each
+  constexpr int ring = Shape<PASS, BM, BN>::RING + (PASS == EXPERT_DW && GATHER ? 8 * 1024 : 0);
   constexpr int stage = 4 * 16 * (BM / 2 * 4 + 16);  // the epilogue: 16 rows of each wave
   return ring > stage ? ring : stage;
 }
@@ -247,11 +252,11 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
   }
 
   // the row indices of gathered k-rows: lane l's of half slab Y at idx0 + (Y % 8)*1024 + 4l
-  const uint32_t idx0 = lds0 + (uint32_t)(2 * Sh::SLAB + wave * 256 + 4 * lane);
+  const uint32_t idx0 = lds0 + (uint32_t)(Sh::RING + wave * 256 + 4 * lane);
   const i32x4 ri = GATHER_W ? buf_rsrc(a.rows + r0, (uint32_t)K * 4u) : i32x4{0, 0, 0, 0};
   auto load_index = [&](int Y) {
     if constexpr (GATHER_W)
-      dma4(ri, (uint32_t)(Y * 32 + kr) * 4u, lds0 + (uint32_t)(2 * Sh::SLAB + wave * 256 + (Y & 7) * 1024));
+      dma4(ri, (uint32_t)(Y * 32 + kr) * 4u, lds0 + (uint32_t)(Sh::RING + wave * 256 + (Y & 7) * 1024));
   };
   auto index_of = [&](int Y) {  // (its indices have landed)
     return *(const __attribute__((address_space(3))) int *)(uintptr_t)(idx0 + (uint32_t)((Y & 7) * 1024));
@@ -270,37 +275,42 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
         if constexpr (!B_KC) wb.r[2] = Y == nhs - 1 ? (int)wb.last : 0;
       }
     }
-    if constexpr ((A_KC || B_KC) && h == 1) {
+    if constexpr ((A_KC && h == 1) || (B_KC && h == Sh::HB)) {
       const int X = Y >> 1;
       if (X >= nsl - 1) {
-        if constexpr (A_KC) wa.r[2] = X == nsl - 1 ? (int)wa.last : 0;
-        if constexpr (B_KC) wb.r[2] = X == nsl - 1 ? (int)wb.last : 0;
         const bool past = kc >= k_last;  // this lane's k lies past the end
-        if constexpr (A_KC)
+        if constexpr (A_KC && h == 1) {
+          wa.r[2] = X == nsl - 1 ? (int)wa.last : 0;
 #pragma unroll
           for (int q = 0; q < Sh::PA; ++q) va[q] = past ? XW_OOB : va[q];
-        if constexpr (B_KC)
+        }
+        if constexpr (B_KC && h == Sh::HB) {
+          wb.r[2] = X == nsl - 1 ? (int)wb.last : 0;
 #pragma unroll
           for (int q = 0; q < Sh::PB; ++q) vb[q] = past ? XW_OOB : vb[q];
+        }
       }
     }
   };
   auto advance = [&](auto htag) {
     constexpr int h = decltype(htag)::value;
     if constexpr ((A_KC && h == 1) || (!A_KC && !GATHER_W)) wa.advance();
-    if constexpr (h == 1 || !B_KC) wb.advance();
+    if constexpr (h == Sh::HB || !B_KC) wb.advance();
   };
+  // B's slots of slabs S, S + 1 and S + 2 (TRI; else they go with A's)
+  uint32_t ub0 = lds0 + 2 * Sh::SA, ub1 = ub0 + Sh::SB, ub2 = ub1 + Sh::SB;
   // piece q of the loads of k-step h into slot t, by f(descriptor, offset, LDS address, instruction's offset)
   auto piece = [&](auto ttag, auto htag, auto qtag, auto f) {
     constexpr int t = decltype(ttag)::value, h = decltype(htag)::value, q = decltype(qtag)::value;
-    constexpr uint32_t slot = (uint32_t)(t * Sh::SLAB);
     if constexpr (q < Sh::la(h)) {
-      if constexpr (A_KC) f(wa.r, va[q], lds0 + (uint32_t)(wave * Sh::PA * 1024) + slot + q * 1024, std::integral_constant<int, 0>{});
-      else f(wa.r, va[0], lds0 + (uint32_t)(wave * 1024) + slot + q * 8192 + h * 4096, std::integral_constant<int, 128 * q>{});
+      constexpr uint32_t to = (uint32_t)(t * Sh::SA);
+      if constexpr (A_KC) f(wa.r, va[q], lds0 + (uint32_t)(wave * Sh::PA * 1024) + to + q * 1024, std::integral_constant<int, 0>{});
+      else f(wa.r, va[0], lds0 + (uint32_t)(wave * 1024) + to + q * 8192 + h * 4096, std::integral_constant<int, 128 * q>{});
     } else {
       constexpr int p = q - Sh::la(h);
-      constexpr uint32_t to = slot + (uint32_t)(BM * 128);
-      if constexpr (B_KC) f(wb.r, vb[p], lds0 + (uint32_t)(wave * Sh::PB * 1024) + to + p * 1024, std::integral_constant<int, 0>{});
+      constexpr uint32_t to = (uint32_t)(2 * Sh::SA + t * Sh::SB);
+      if constexpr (Sh::TRI) f(wb.r, vb[p], ub2 + (uint32_t)(wave * Sh::PB * 1024) + p * 1024, std::integral_constant<int, 0>{});
+      else if constexpr (B_KC) f(wb.r, vb[p], lds0 + (uint32_t)(wave * Sh::PB * 1024) + to + p * 1024, std::integral_constant<int, 0>{});
       else f(wb.r, vb[0], lds0 + (uint32_t)(wave * 1024) + to + p * 8192 + h * 4096, std::integral_constant<int, 128 * p>{});
     }
   };
@@ -308,25 +318,27 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
   // ---- fragments
   const int fi = lane & 15, kg = lane >> 4, wm = wave & 1, wn = wave >> 1;
   const int tr = 8 * kg + (fi >> 2);
-  // addresses of k-step 0 (k contiguous: and of k-step 1) of slot 0, then those of slot 1: the rest of a read's
-  // address is a constant of the instruction
+  // addresses of k-step 0 (k contiguous: and of k-step 1) of slot 0, then those of slot 1 (TRI: B's without the
+  // slot): the rest of a read's address is a constant of the instruction
   constexpr int NA = A_KC ? 2 : 4, NB = B_KC ? 2 : 4;
   uint32_t fa[2][NA], fb[2][NB];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t slot = lds0 + (uint32_t)(t * Sh::SLAB);
       const uint32_t kcl = (uint32_t)(fi * 128 + (((4 * j + kg) ^ (fi & 7)) * 16));
       const uint32_t trr = (uint32_t)(((2 * j + ((fi >> 1) & 1)) ^ xw_swz_tr(tr)) * 16 + tr * 128 + 8 * (fi & 1));
-      if (j < NA) fa[t][j] = slot + (A_KC ? (uint32_t)(wm * FM * 2048) + kcl : (uint32_t)(wm * FM / 4 * 8192) + trr);
+      if (j < NA)
+        fa[t][j] = lds0 + (uint32_t)(t * Sh::SA) + (A_KC ? (uint32_t)(wm * FM * 2048) + kcl : (uint32_t)(wm * FM / 4 * 8192) + trr);
       if (j < NB)
-        fb[t][j] = slot + (uint32_t)(BM * 128) + (B_KC ? (uint32_t)(wn * FN * 2048) + kcl : (uint32_t)(wn * FN / 4 * 8192) + trr);
+        fb[t][j] = (Sh::TRI ? 0u : lds0 + (uint32_t)(2 * Sh::SA + t * Sh::SB)) +
+                   (B_KC ? (uint32_t)(wn * FN * 2048) + kcl : (uint32_t)(wn * FN / 4 * 8192) + trr);
     }
 #pragma unroll
     for (int j = 0; j < NA; ++j) asm volatile("" : "+v"(fa[t][j]));
 #pragma unroll
-    for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(fb[t][j]));
+    for (int j = 0; j < NB; ++j)
+      if (!Sh::TRI || t == 0) asm volatile("" : "+v"(fb[t][j]));
   }
   static_assert(FM % 4 == 0 && FN % 4 == 0, "k-row fragments come in whole quarters");
   auto lds16 = [](uint32_t p) {
@@ -344,7 +356,7 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     else return lds_tr(fa[t][i & 3] + (uint32_t)((i >> 2) * 8192 + h * 4096));
   };
   auto read_b = [&](int t, int h, int j) {
-    if constexpr (B_KC) return lds16(fb[t][h] + (uint32_t)(j * 2048));
+    if constexpr (B_KC) return lds16(fb[t][h] + (uint32_t)(j * 2048));  // (not TRI)
     else return lds_tr(fb[t][j & 3] + (uint32_t)((j >> 2) * 8192 + h * 4096));
   };
 
@@ -372,6 +384,7 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     constexpr int t = decltype(ttag)::value, h = decltype(htag)::value;
     if constexpr (GATHER_W) gather(2 * t + h, index_of(2 * t + h));
     ends(2 * t + h, htag);
+    if constexpr (Sh::TRI && h == 0) ub2 = t ? ub1 : ub0;
     static_for<Sh::loads(h)>([&](auto q) {
       piece(ttag, htag, q,
             [&](const i32x4 &r, uint32_t voff, uint32_t to, auto imm) { dma16_at<decltype(imm)::value>(r, voff, to); });
@@ -384,6 +397,7 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
   load_index(6);  // (again: every k-step's loads end with one)
   first(c1, c1);
   load_index(7);
+  if constexpr (Sh::TRI) ub2 = ub1 + Sh::SB;
   // loads that may be under way when k-step h begins. Its fragment reads take a half slab loaded three k-steps ago,
   // for h = 1 a k-contiguous operand's slab loaded two ago.
   constexpr int IDX = GATHER_W ? 1 : 0;
@@ -395,7 +409,7 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
 #pragma unroll
   for (int i = 0; i < FM; ++i) av[0][i] = read_a(0, 0, i);
 #pragma unroll
-  for (int j = 0; j < FN; ++j) bv[0][j] = read_b(0, 0, j);
+  for (int j = 0; j < FN; ++j) bv[0][j] = Sh::TRI ? lds16(ub0 + fb[0][0] + (uint32_t)(j * 2048)) : read_b(0, 0, j);
   if constexpr (GATHER_W) gather(4, index_of(4));
   ends(4, c0);
 
@@ -409,6 +423,11 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     else step_wait<true, VM1>();
     const int Y = 2 * S + h;
     int row = 0;
+    uint32_t pb = 0;
+    if constexpr (Sh::TRI) {  // B's fragments of the next k-step
+      pb = (h == 0 ? ub0 : ub1) + fb[0][(h ^ 1) % NB];
+      asm volatile("" : "+v"(pb));
+    }
     constexpr int NM = FM * FN, NR = FM + FN, NL = Sh::loads(h), SPAN = NM < 3 * NL ? NM : 3 * NL;
     static_assert(NM >= 2 * NR + 8 && SPAN >= 2 * NL, "");
     static_for<NM>([&](auto ptag) {
@@ -422,6 +441,7 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
       constexpr int at = r < both ? r / 2 : r - both / 2;
       if constexpr (r < NR) {
         if constexpr (is_a) av[h ^ 1][at] = read_a(h == 0 ? t : t ^ 1, h ^ 1, at);
+        else if constexpr (Sh::TRI) bv[h ^ 1][at] = lds16(pb + (uint32_t)(at * 2048));
         else bv[h ^ 1][at] = read_b(h == 0 ? t : t ^ 1, h ^ 1, at);
       }
       // load q with an even product
@@ -441,6 +461,12 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
         }
       }
       if constexpr (GATHER_W && p == NM - 6) gather(Y + 5, row);
+      if constexpr (Sh::TRI && h == 1 && p == NM - 8) {
+        const uint32_t u = ub0;
+        ub0 = ub1;
+        ub1 = ub2;
+        ub2 = u;
+      }
       if constexpr (p == NM - 3) ends(Y + 5, std::integral_constant<int, h ^ 1>{});
       __builtin_amdgcn_sched_barrier(0);
     });
