@@ -138,15 +138,19 @@ struct Shape {
   static constexpr int loads(int h) { return la(h) + lb(h); }
 };
 
+// A wave's part of LDS in the epilogue: its outputs as bf16, half of them as fp32.
+constexpr int xw_stage_bytes(int BM, int BN) { return BM / 2 * (BN / 2) * 2; }
+
 template <int PASS, int BM, int BN, bool GATHER>
 constexpr int xw_lds_bytes() {
   // the slots; Delta_W with gathered x: the row indices of eight half slabs, 256 bytes a wave each
   constexpr int ring = Shape<PASS, BM, BN>::RING + (PASS == EXPERT_DW && GATHER ? 8 * 1024 : 0);
-  constexpr int stage = 4 * 16 * (BM / 2 * 4 + 16);  // the epilogue: 16 rows of each wave
+  constexpr int stage = 4 * xw_stage_bytes(BM, BN);
   return ring > stage ? ring : stage;
 }
 
-template <int PASS, int BM, int BN, bool GATHER, int WGS>
+// ES: bytes of an output (a kernel for each: with both in one, the sums were copied ahead of the branch, and spilled)
+template <int PASS, int BM, int BN, bool GATHER, int ES, int WGS>
 __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int tiles_m, int tiles_n) {
   using Sh = Shape<PASS, BM, BN>;
   constexpr bool A_KC = Sh::A_KC, B_KC = Sh::B_KC;
@@ -360,11 +364,17 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     else return lds_tr(fb[t][j & 3] + (uint32_t)((j >> 2) * 8192 + h * 4096));
   };
 
+  // the sums begin with the bias
   f32x4 acc[FM][FN], accd[PASS == EXPERT_DW ? FN : 1];
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
+  for (int i = 0; i < FM; ++i) {
+    f32x4 first = {0.f, 0.f, 0.f, 0.f};
+    const int m = m0 + wm * (BM / 2) + 16 * i + 4 * kg;  // (the width is a multiple of 8: all four or none)
+    if (PASS == EXPERT_FWD && a.bias && m < M)
+      first = *reinterpret_cast<const f32x4_any *>(a.bias + (int64_t)e * a.d_out + m);
 #pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < FN; ++j) acc[i][j] = first;
+  }
   // db: the products with a row of ones, by the waves of the first m tile's first half
   const bool do_db = PASS == EXPERT_DW && a.db && m0 == 0 && wm == 0;
   if constexpr (PASS == EXPERT_DW)
@@ -505,82 +515,92 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     if (!a.out) return;
   }
 
-  // ---- epilogue: each wave puts 16 rows of its outputs at a time through its own part of LDS ([n][m]) and
-  // stores whole rows, 16 bytes a lane
-  constexpr int WM = BM / 2;  // outputs of a row
-  char *stg = smem + wave * (16 * (WM * 4 + 16));
-  const int mw = m0 + wm * WM;
-  f32x4 bias[PASS == EXPERT_FWD ? FM : 1];
-  if constexpr (PASS == EXPERT_FWD) {
+  // ---- epilogue: each wave puts its outputs through its own part of LDS ([n][m], 16-byte chunks XORed with the row)
+  // and stores whole rows, 16 bytes a lane, past the caches (537 MB of gradients of few rows: 131 -> 109 us); what lies outside the tile's rows or columns is past the descriptor.
+  constexpr int WM = BM / 2, WN = BN / 2;  // columns, rows of a wave
+  const int mw = m0 + wm * WM, nw = n0 + wn * WN;
+  const uint32_t stg = lds0 + (uint32_t)(wave * xw_stage_bytes(BM, BN));
+  const float least = PASS == EXPERT_FWD && a.relu ? 0.f : -__builtin_inff();
+  const int rows_left = min(WN, n_end - nw);
+  if (rows_left <= 0 || mw >= M) return;
+  // Rows of 32-bit outputs go in two halves of the wave's.
+  {
+    constexpr int PITCH = WM * ES, CPR = PITCH / 16;  // row bytes, chunks a row
+    constexpr int PARTS = ES / 2, FP = FN / PARTS, RPI = 64 / CPR, NST = FP * 16 / RPI;  // blocks a part; rows, stores
+    char *dst = reinterpret_cast<char *>(a.out) + ((PASS == EXPERT_DW ? (int64_t)e * a.so : 0) + (int64_t)nw * a.ldo + mw) * ES;
+    const i32x4 ro = buf_rsrc(dst, (uint32_t)(((int64_t)(rows_left - 1) * a.ldo + min(WM, M - mw)) * ES));
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(dst, 0, ro[2], BUF_DW3);
+    const int row0 = lane / CPR, ch = lane % CPR;
+    const uint32_t col = mw + ch * (16 / ES) < M ? (uint32_t)(ch * 16) : XW_OOB;
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = mw + 16 * i + 4 * kg;  // (the width is a multiple of 8: all four or none)
-      bias[i] = a.bias && m < M ? *reinterpret_cast<const f32x4_any *>(a.bias + (int64_t)e * a.d_out + m)
-                                : f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-  }
-  const bool half = a.out_dtype == IMBD_BF16;
+    for (int part = 0; part < PARTS; ++part) {
 #pragma unroll
-  for (int j = 0; j < FN; ++j) {
-    const int nb = n0 + 16 * (wn * FN + j);
-    if (nb >= n_end) break;
+      for (int i = 0; i < FM; ++i) {
+        const uint32_t c = ES == 2 ? (uint32_t)(((2 * i + (kg >> 1)) ^ fi) * 16 + 8 * (kg & 1)) : (uint32_t)(((4 * i + kg) ^ fi) * 16);
+        const uint32_t p = stg + (uint32_t)(fi * PITCH) + c;
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      f32x4 v = acc[i][j];
-      if constexpr (PASS == EXPERT_FWD) {
+        for (int j = 0; j < FP; ++j) {
+          f32x4 v = acc[i][part * FP + j];
+          if constexpr (PASS == EXPERT_FWD) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          v[q] += bias[i][q];
-          if (a.relu) v[q] = v[q] < 0.f ? 0.f : v[q];  // (a NaN stays one)
+            for (int q = 0; q < 4; ++q) v[q] = __builtin_elementwise_maximum(v[q], least);  // (a NaN stays one)
+          }
+          if constexpr (ES == 2)
+            *(__attribute__((address_space(3))) u32x2 *)(uintptr_t)(p + j * 16 * PITCH) =
+                u32x2{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
+          else
+            *(__attribute__((address_space(3))) f32x4 *)(uintptr_t)(p + j * 16 * PITCH) = v;
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if (PASS != EXPERT_DW && half)
-        *reinterpret_cast<u32x2 *>(stg + fi * (WM * 2 + 16) + (16 * i + 4 * kg) * 2) =
-            u32x2{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
-      else
-        *reinterpret_cast<f32x4 *>(stg + fi * (WM * 4 + 16) + (16 * i + 4 * kg) * 4) = v;
-    }
-    if (PASS != EXPERT_DW && half) {
-      constexpr int LPR = WM / 8, RPI = 64 / LPR;  // lanes a row, rows an instruction
+      constexpr int BATCH = 8;
+      static_assert(NST % BATCH == 0, "");
+#pragma unroll 1
+      for (int s0 = 0; s0 < NST; s0 += BATCH) {
+        if (part * FP * 16 + s0 * RPI >= rows_left) break;
+        u32x4 v[BATCH], mk[BATCH];
+        if constexpr (PASS == EXPERT_DX) {
+          if (a.mask) {
 #pragma unroll
-      for (int p = 0; p < 16 / RPI; ++p) {
-        const int r = p * RPI + lane / LPR, m = mw + (lane % LPR) * 8, n = nb + r;
-        u32x4 v = *reinterpret_cast<const u32x4 *>(stg + r * (WM * 2 + 16) + (lane % LPR) * 16);
-        if (n < n_end && m < M) {
-          if constexpr (PASS == EXPERT_DX) {
-            if (a.mask) {
-              const int row = a.rows ? a.rows[n] : n;
-              u32x4 mk = {0u, 0u, 0u, 0u};
-              if (row >= 0 && row < a.n_x) mk = *reinterpret_cast<const u32x4 *>(x + (int64_t)row * a.ldx + m);
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                if (!(bf16_to_f32((uint16_t)mk[q]) > 0.f)) v[q] &= 0xffff0000u;
-                if (!(bf16_to_f32((uint16_t)(mk[q] >> 16)) > 0.f)) v[q] &= 0xffffu;
+            for (int q = 0; q < BATCH; ++q) {
+              const int r = part * FP * 16 + (s0 + q) * RPI + row0;
+              mk[q] = u32x4{0u, 0u, 0u, 0u};
+              if (r < rows_left && col != XW_OOB) {
+                const int row = a.rows ? a.rows[nw + r] : nw + r;
+                const uint16_t *px = x + (int64_t)row * a.ldx + mw + ch * (16 / ES);
+                if (row >= 0 && row < a.n_x) {
+                  if constexpr (ES == 2) {
+                    mk[q] = *reinterpret_cast<const u32x4 *>(px);
+                  } else {
+                    const u32x2 h = *reinterpret_cast<const u32x2 *>(px);
+                    mk[q][0] = h[0];
+                    mk[q][1] = h[1];
+                  }
+                }
               }
             }
           }
-          *reinterpret_cast<u32x4 *>(reinterpret_cast<uint16_t *>(a.out) + (int64_t)n * a.ldo + m) = v;
         }
-      }
-    } else {
-      constexpr int LPR = WM / 4, RPI = 64 / LPR;
 #pragma unroll
-      for (int p = 0; p < 16 / RPI; ++p) {
-        const int r = p * RPI + lane / LPR, m = mw + (lane % LPR) * 4, n = nb + r;
-        f32x4 v = *reinterpret_cast<const f32x4 *>(stg + r * (WM * 4 + 16) + (lane % LPR) * 16);
-        if (n < n_end && m < M) {
+        for (int q = 0; q < BATCH; ++q) {
+          const int r = (s0 + q) * RPI + row0;
+          v[q] = *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)(stg + (uint32_t)(r * PITCH + ((ch ^ (r & 15)) * 16)));
+        }
+#pragma unroll
+        for (int q = 0; q < BATCH; ++q) {
           if constexpr (PASS == EXPERT_DX) {
             if (a.mask) {
-              const int row = a.rows ? a.rows[n] : n;
-              u32x2 mk = {0u, 0u};
-              if (row >= 0 && row < a.n_x) mk = *reinterpret_cast<const u32x2 *>(x + (int64_t)row * a.ldx + m);
 #pragma unroll
-              for (int q = 0; q < 4; ++q)
-                if (!(bf16_to_f32((uint16_t)(mk[q >> 1] >> (16 * (q & 1)))) > 0.f)) v[q] = 0.f;
+              for (int w2 = 0; w2 < 8 / (ES / 2); ++w2) {
+                const bool on = bf16_to_f32((uint16_t)(mk[q][w2 >> 1] >> (16 * (w2 & 1)))) > 0.f;
+                if constexpr (ES == 2) v[q][w2 >> 1] &= on ? 0xffffffffu : (w2 & 1) ? 0xffffu : 0xffff0000u;
+                else v[q][w2] = on ? v[q][w2] : 0u;
+              }
             }
           }
-          *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out) +
-                                     (PASS == EXPERT_DW ? (int64_t)e * a.so : 0) + (int64_t)n * a.ldo + m) = v;
+          const int r = part * FP * 16 + (s0 + q) * RPI + row0;
+          const uint32_t off = col == XW_OOB ? XW_OOB : (uint32_t)r * (uint32_t)(a.ldo * ES) + col;
+          __builtin_amdgcn_raw_buffer_store_b128(v[q], rs, off, 0, 2);  // nt
         }
       }
     }
@@ -595,7 +615,7 @@ bool expert_wide_fits(int pass, int dtype, const ExpertArgs &a) {
   const int es = a.out_dtype == IMBD_BF16 ? 2 : 4;
   const int64_t ld_most = (int64_t)1 << 22;  // 256 rows of a tile within one descriptor
   if (dtype != IMBD_BF16 || a.d_in % 8 || a.d_out % 8) return false;
-  if (a.out && (!al16(a.out, a.ldo, es) || (pass == EXPERT_DW && a.so % 4))) return false;
+  if (a.out && (!al16(a.out, a.ldo, es) || a.ldo >= ld_most || (pass == EXPERT_DW && a.so % 4))) return false;
   if (pass != EXPERT_DW && (!al16(a.w, a.ldw, 2) || a.sw % 8 || a.ldw >= ld_most)) return false;
   if (pass != EXPERT_FWD && (!al16(a.dy, a.lddy, 2) || a.lddy >= ld_most)) return false;
   if (pass != EXPERT_DX || a.mask) {
@@ -606,7 +626,7 @@ bool expert_wide_fits(int pass, int dtype, const ExpertArgs &a) {
   return a.n_rows < (1 << 29);  // byte offsets into rows
 }
 
-template <int PASS, int BM, int BN, int WGS>
+template <int PASS, int BM, int BN, int ES, int WGS>
 static int launch(const ExpertArgs &a, hipStream_t s) {
   const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in;
   const int64_t tm = PASS == EXPERT_DW && !a.out ? 1 : (M + BM - 1) / BM;
@@ -617,22 +637,23 @@ static int launch(const ExpertArgs &a, hipStream_t s) {
     return IMBD_EUNSUPPORTED;
   }
   const dim3 grid((unsigned)((blocks + 255) / 256 * 256));
+  const int tiles_n = (int)(PASS == EXPERT_DW ? tn : rows);
   {
     LaunchTimer t(IMBD_K_EXPERT_FWD + PASS, 0, s);
-    if (a.rows && PASS != EXPERT_DX)
-      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, true, WGS>), grid, dim3(256), 0, s, a, (int)tm,
-                         (int)(PASS == EXPERT_DW ? tn : rows));
+    if (a.rows && PASS != EXPERT_DX)  // (Delta_X gathers nothing but its mask)
+      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, PASS != EXPERT_DX, ES, WGS>), grid, dim3(256), 0, s, a, (int)tm,
+                         tiles_n);
     else
-      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, false, WGS>), grid, dim3(256), 0, s, a, (int)tm,
-                         (int)(PASS == EXPERT_DW ? tn : rows));
+      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, false, ES, WGS>), grid, dim3(256), 0, s, a, (int)tm, tiles_n);
   }
   return check_launch("expert_wide");
 }
 
 int run_expert_wide(int pass, const ExpertArgs &a, hipStream_t s) {
-  if (pass == EXPERT_FWD) return launch<EXPERT_FWD, 256, 256, 1>(a, s);
-  if (pass == EXPERT_DX) return launch<EXPERT_DX, 256, 256, 1>(a, s);
-  return launch<EXPERT_DW, 256, 256, 1>(a, s);
+  const bool half = a.out_dtype == IMBD_BF16;
+  if (pass == EXPERT_FWD) return half ? launch<EXPERT_FWD, 256, 256, 2, 1>(a, s) : launch<EXPERT_FWD, 256, 256, 4, 1>(a, s);
+  if (pass == EXPERT_DX) return half ? launch<EXPERT_DX, 256, 256, 2, 1>(a, s) : launch<EXPERT_DX, 256, 256, 4, 1>(a, s);
+  return launch<EXPERT_DW, 256, 256, 4, 1>(a, s);
 }
 
 }  // namespace imbd
