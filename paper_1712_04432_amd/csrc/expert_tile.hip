@@ -7,12 +7,15 @@
 //   forward: m = o, n = s, k = i (both operands k-contiguous); Delta_X: m = i, n = s, k = o (W by k-rows);
 //   Delta_W: m = i, n = o, k = s (both by k-rows).
 //
-// A workgroup of four waves owns a 64 x 64 tile of D and walks K in steps of 128 bytes a row,
-// double-buffered in LDS with the next step's loads in flight over the products; rows of 144 bytes make
-// every fragment one conflict-free 16-byte read. Operands stored by k-rows are transposed in registers on
-// their way. Loads are 16 bytes at any element alignment, the chunks that an edge cuts go element by
-// element, and addresses are 64-bit, so no size or stride is special. fp32 operands run on the fp32 matrix
-// instruction: products and sums are fp32 for both types.
+// A workgroup of four waves owns a 64 x 64 tile of D and walks K in steps of 128 bytes a row, double-buffered
+// in LDS, with the loads of the next two steps in flight over the products; rows of 144 bytes make every
+// fragment one conflict-free 16-byte read. Operands stored by k-rows are transposed in registers on their way.
+// Addresses are 64-bit and loads are 16 bytes at any element alignment, so no size or stride is special. Whole
+// steps load without conditions (rows that do not count from a row that exists); the last step of a K that is
+// no whole number of them, and k-rows at the edge of their matrix, chunk by chunk and element by element.
+// fp32 operands run on the fp32 matrix instruction: products and sums are fp32 for both types.
+
+#include <type_traits>
 
 #include "expert.h"
 
@@ -39,26 +42,37 @@ __device__ __forceinline__ u32x4 chunk16(const T *p, int valid) {
 }
 
 // k-contiguous operand: 64 rows x 128 bytes, two chunks a thread. row(r) gives row r's first element, or
-// null for a row of zeros; it does not change over k.
+// null for a row of zeros; it does not change over k. `some`: any row that exists.
 template <typename T>
 struct KcTile {
   static constexpr int VEC = 16 / (int)sizeof(T);
   const T *p[2];
-  u32x4 v[2];
+  bool ok[2];
+  u32x4 v[2][2];  // [register set][chunk]
   template <typename F>
-  __device__ __forceinline__ void init(F row, int tid) {
+  __device__ __forceinline__ void init(F row, const T *some, int tid) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) p[i] = row((tid + 256 * i) >> 3);
+    for (int i = 0; i < 2; ++i) {
+      p[i] = row((tid + 256 * i) >> 3);
+      ok[i] = p[i] != nullptr;
+      if (!ok[i]) p[i] = some;
+    }
   }
-  __device__ __forceinline__ void load(int k0, int K, int tid) {
+  // G: with the edges looked at
+  template <bool G>
+  __device__ __forceinline__ void load(int set, int k0, int K, int tid) {
     const int kk = k0 + (tid & 7) * VEC;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) v[i] = p[i] && kk < K ? chunk16<T>(p[i] + kk, K - kk) : u32x4{0u, 0u, 0u, 0u};
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (G) v[set][i] = ok[i] && kk < K ? chunk16<T>(p[i] + kk, K - kk) : u32x4{0u, 0u, 0u, 0u};
+      else v[set][i] = *reinterpret_cast<const u32x4_any *>(p[i] + kk);
+    }
   }
-  __device__ __forceinline__ void store(char *lds, int tid) {
+  __device__ __forceinline__ void store(int set, char *lds, int tid) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      *reinterpret_cast<u32x4 *>(lds + ((tid + 256 * i) >> 3) * XT_PITCH + (tid & 7) * 16) = v[i];
+      *reinterpret_cast<u32x4 *>(lds + ((tid + 256 * i) >> 3) * XT_PITCH + (tid & 7) * 16) =
+          ok[i] ? v[set][i] : u32x4{0u, 0u, 0u, 0u};
   }
 };
 
@@ -69,18 +83,24 @@ template <typename T>
 struct TrTile {
   static constexpr int VEC = 16 / (int)sizeof(T);
   static constexpr int NB = 8 * XT / VEC;
-  u32x4 v[VEC];
-  template <typename F>
-  __device__ __forceinline__ void load(F krow, int k0, int K, int cols, int tid) {
+  u32x4 v[2][VEC];
+  template <bool G, typename F>
+  __device__ __forceinline__ void load(int set, F krow, const T *some, int k0, int K, int cols, int tid) {
     if (tid >= NB) return;
     const int kb = k0 + (tid & 7) * VEC, c = (tid >> 3) * VEC;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
-      const T *p = kb + j < K && c < cols ? krow(kb + j) : nullptr;
-      v[j] = p ? chunk16<T>(p + c, cols - c) : u32x4{0u, 0u, 0u, 0u};
+      if constexpr (G) {
+        const T *p = kb + j < K && c < cols ? krow(kb + j) : nullptr;
+        v[set][j] = p ? chunk16<T>(p + c, cols - c) : u32x4{0u, 0u, 0u, 0u};
+      } else {
+        const T *p = krow(kb + j);
+        v[set][j] = *reinterpret_cast<const u32x4_any *>((p ? p : some) + c);
+        if (!p) v[set][j] = u32x4{0u, 0u, 0u, 0u};
+      }
     }
   }
-  __device__ __forceinline__ void store(char *lds, int tid) {
+  __device__ __forceinline__ void store(int set, char *lds, int tid) {
     if (tid >= NB) return;
 #pragma unroll
     for (int r = 0; r < VEC; ++r) {
@@ -88,10 +108,10 @@ struct TrTile {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         if constexpr (VEC == 8) {
-          const uint32_t x = v[2 * q][r >> 1], y = v[2 * q + 1][r >> 1];
+          const uint32_t x = v[set][2 * q][r >> 1], y = v[set][2 * q + 1][r >> 1];
           o[q] = (r & 1) ? ((x >> 16) | (y & 0xffff0000u)) : ((x & 0xffffu) | (y << 16));
         } else {
-          o[q] = v[q][r];
+          o[q] = v[set][q][r];
         }
       }
       *reinterpret_cast<u32x4 *>(lds + ((tid >> 3) * VEC + r) * XT_PITCH + (tid & 7) * 16) = o;
@@ -141,26 +161,33 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
   KcTile<T> ka, kb;
   TrTile<T> ta, tb;
   const int tid_b = tid ^ 128;  // (the k-row operand of n: the other half of the workgroup)
+  // whether whole steps of k-rows may load without conditions: the tile's columns all exist
+  bool inside = true;
   if constexpr (PASS == EXPERT_FWD) {
-    ka.init([&](int r) { return m0 + r < M ? w + (int64_t)(m0 + r) * a.ldw : nullptr; }, tid);
-    kb.init([&](int r) { return n0 + r < n_end ? x_row(n0 + r) : nullptr; }, tid);
+    ka.init([&](int r) { return m0 + r < M ? w + (int64_t)(m0 + r) * a.ldw : nullptr; }, w, tid);
+    kb.init([&](int r) { return n0 + r < n_end ? x_row(n0 + r) : nullptr; }, a.n_x > 0 ? x : w, tid);
   } else if constexpr (PASS == EXPERT_DX) {
-    kb.init([&](int r) { return n0 + r < n_end ? dy + (int64_t)(n0 + r) * a.lddy : nullptr; }, tid);
+    kb.init([&](int r) { return n0 + r < n_end ? dy + (int64_t)(n0 + r) * a.lddy : nullptr; }, dy, tid);
+    inside = m0 + XT <= M;
+  } else {
+    inside = m0 + XT <= M && n0 + XT <= n_end && a.n_x > 0 && x != nullptr;
   }
-  auto load = [&](int k0) {
-    if constexpr (PASS == EXPERT_FWD) ka.load(k0, K, tid);
-    if constexpr (PASS != EXPERT_DW) kb.load(k0, K, tid);
-    if constexpr (PASS == EXPERT_DX) ta.load([&](int k) { return w + (int64_t)k * a.ldw + m0; }, k0, K, M - m0, tid);
+  auto load = [&](auto gtag, int set, int k0) {
+    constexpr bool G = decltype(gtag)::value;
+    if constexpr (PASS == EXPERT_FWD) ka.template load<G>(set, k0, K, tid);
+    if constexpr (PASS != EXPERT_DW) kb.template load<G>(set, k0, K, tid);
+    if constexpr (PASS == EXPERT_DX)
+      ta.template load<G>(set, [&](int k) { return w + (int64_t)k * a.ldw + m0; }, w, k0, K, M - m0, tid);
     if constexpr (PASS == EXPERT_DW) {
-      ta.load([&](int k) { const T *p = x_row(r0 + k); return p ? p + m0 : nullptr; }, k0, K, M - m0, tid);
-      tb.load([&](int k) { return dy + (int64_t)(r0 + k) * a.lddy + n0; }, k0, K, n_end - n0, tid_b);
+      ta.template load<G>(set, [&](int k) { const T *p = x_row(r0 + k); return p ? p + m0 : nullptr; }, x + m0, k0, K, M - m0, tid);
+      tb.template load<G>(set, [&](int k) { return dy + (int64_t)(r0 + k) * a.lddy + n0; }, dy, k0, K, n_end - n0, tid_b);
     }
   };
-  auto store = [&](char *buf) {
-    if constexpr (PASS == EXPERT_FWD) ka.store(buf, tid);
-    else ta.store(buf, tid);
-    if constexpr (PASS != EXPERT_DW) kb.store(buf + XT * XT_PITCH, tid);
-    else tb.store(buf + XT * XT_PITCH, tid_b);
+  auto store = [&](int set, char *buf) {
+    if constexpr (PASS == EXPERT_FWD) ka.store(set, buf, tid);
+    else ta.store(set, buf, tid);
+    if constexpr (PASS != EXPERT_DW) kb.store(set, buf + XT * XT_PITCH, tid);
+    else tb.store(set, buf + XT * XT_PITCH, tid_b);
   };
 
   const int wm = (wave & 1) * 32, wn = (wave >> 1) * 32, fr = lane & 15, fg = lane >> 4;
@@ -172,15 +199,15 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
   const bool do_db = PASS == EXPERT_DW && a.db && tm == 0;
   float dbsum = 0.f;
 
-  const int nk = (K + BK - 1) / BK;
-  if (nk > 0) {
-    load(0);
-    store(smem);
-  }
-  __syncthreads();
-  for (int kt = 0; kt < nk; ++kt) {
+  const int nk = (K + BK - 1) / BK, nw = inside ? K / BK : 0;  // steps; whole ones
+  const std::integral_constant<bool, false> plain{};
+  const std::integral_constant<bool, true> guarded{};
+  auto fetch = [&](int set, int kt) {
+    if (kt < nw) load(plain, set, kt * BK);
+    else if (kt < nk) load(guarded, set, kt * BK);
+  };
+  auto compute = [&](int kt) {
     const char *sa = smem + (kt & 1) * XT_STAGE, *sb = sa + XT * XT_PITCH;
-    if (kt + 1 < nk) load((kt + 1) * BK);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
       u32x4 fa[2], fb[2];
@@ -223,7 +250,22 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
         }
       }
     }
-    if (kt + 1 < nk) store(smem + ((kt + 1) & 1) * XT_STAGE);
+  };
+  // step kt computes from LDS buffer kt % 2 while the loads of kt + 1 (set 1 - kt % 2, stored at its end) and
+  // kt + 2 (the other set) are in flight
+  fetch(0, 0);
+  fetch(1, 1);
+  if (nk > 0) store(0, smem);
+  __syncthreads();
+  for (int kt = 0; kt < nk; kt += 2) {
+    fetch(0, kt + 2);
+    compute(kt);
+    if (kt + 1 < nk) store(1, smem + XT_STAGE);
+    __syncthreads();
+    if (kt + 1 >= nk) break;
+    fetch(1, kt + 3);
+    compute(kt + 1);
+    if (kt + 2 < nk) store(0, smem);
     __syncthreads();
   }
   if (do_db) {

@@ -25,6 +25,7 @@
 // zero: by lane (an offset past the buffer descriptor) or because the descriptor ends there. An expert's
 // neighbours never enter a sum, not even times zero: their rows may hold infinities.
 
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -439,7 +440,8 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
       asm volatile("" : "+v"(pb));
     }
     constexpr int NM = FM * FN, NR = FM + FN, NL = Sh::loads(h), SPAN = NM < 3 * NL ? NM : 3 * NL;
-    static_assert(NM >= 2 * NR + 8 && SPAN >= 2 * NL, "");
+    constexpr int ADV = SPAN > NM - 14 ? SPAN : NM - 14;  // behind the last load
+    static_assert(NM >= 2 * NR + 8 && SPAN >= 2 * NL && ADV <= NM - 8, "");
     static_for<NM>([&](auto ptag) {
       constexpr int p = decltype(ptag)::value;
       f32x4 &d = acc[p / FN][p % FN];
@@ -463,7 +465,7 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
       } else {
         mfma(d, ma, mb);
       }
-      if constexpr (p == NM - 14) {
+      if constexpr (p == ADV) {
         advance(htag);
         if constexpr (GATHER_W) {
           load_index(Y + 8);  // (landed three k-steps on, read one after that)
@@ -496,10 +498,6 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
   }
   vm_barrier<0>();  // LDS is free: nothing is in flight and every wave is done reading
   mfma_drain();
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) asm volatile("" : "+a"(acc[i][j]));  // (read behind the wait states)
   if constexpr (PASS == EXPERT_DW)
 #pragma unroll
     for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(accd[j]));
@@ -532,6 +530,27 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(dst, 0, ro[2], BUF_DW3);
     const int row0 = lane / CPR, ch = lane % CPR;
     const uint32_t col = mw + ch * (16 / ES) < M ? (uint32_t)(ch * 16) : XW_OOB;
+    constexpr int BATCH = 8, NBT = NST / BATCH;  // stores in batches
+    static_assert(NST % BATCH == 0, "");
+    // the mask of a batch (Delta_X), loaded ahead of the one before it
+    using MaskVec = typename std::conditional<ES == 2, u32x4, u32x2>::type;  // of as many elements as a store has
+    MaskVec mk[2][BATCH];
+    auto load_mask = [&](int g) {
+      if constexpr (PASS == EXPERT_DX) {
+        if (a.mask && g < PARTS * NBT) {
+#pragma unroll
+          for (int q = 0; q < BATCH; ++q) {
+            const int r = (g * BATCH + q) * RPI + row0;
+            int row = -1;
+            if (r < rows_left && col != XW_OOB) row = a.rows ? a.rows[nw + r] : nw + r;
+            mk[g & 1][q] = MaskVec{};
+            if (row >= 0 && row < a.n_x)
+              mk[g & 1][q] = *reinterpret_cast<const MaskVec *>(x + (int64_t)row * a.ldx + mw + ch * (16 / ES));
+          }
+        }
+      }
+    };
+    load_mask(0);
 #pragma unroll
     for (int part = 0; part < PARTS; ++part) {
 #pragma unroll
@@ -541,6 +560,7 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
 #pragma unroll
         for (int j = 0; j < FP; ++j) {
           f32x4 v = acc[i][part * FP + j];
+          asm volatile("" : "+a"(v));  // (read here, behind the wait states)
           if constexpr (PASS == EXPERT_FWD) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] = __builtin_elementwise_maximum(v[q], least);  // (a NaN stays one)
@@ -553,34 +573,11 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      constexpr int BATCH = 8;
-      static_assert(NST % BATCH == 0, "");
-#pragma unroll 1
-      for (int s0 = 0; s0 < NST; s0 += BATCH) {
-        if (part * FP * 16 + s0 * RPI >= rows_left) break;
-        u32x4 v[BATCH], mk[BATCH];
-        if constexpr (PASS == EXPERT_DX) {
-          if (a.mask) {
 #pragma unroll
-            for (int q = 0; q < BATCH; ++q) {
-              const int r = part * FP * 16 + (s0 + q) * RPI + row0;
-              mk[q] = u32x4{0u, 0u, 0u, 0u};
-              if (r < rows_left && col != XW_OOB) {
-                const int row = a.rows ? a.rows[nw + r] : nw + r;
-                const uint16_t *px = x + (int64_t)row * a.ldx + mw + ch * (16 / ES);
-                if (row >= 0 && row < a.n_x) {
-                  if constexpr (ES == 2) {
-                    mk[q] = *reinterpret_cast<const u32x4 *>(px);
-                  } else {
-                    const u32x2 h = *reinterpret_cast<const u32x2 *>(px);
-                    mk[q][0] = h[0];
-                    mk[q][1] = h[1];
-                  }
-                }
-              }
-            }
-          }
-        }
+      for (int b = 0; b < NBT; ++b) {
+        const int g = part * NBT + b, s0 = b * BATCH;
+        load_mask(g + 1);
+        u32x4 v[BATCH];
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) {
           const int r = (s0 + q) * RPI + row0;
@@ -592,7 +589,7 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
             if (a.mask) {
 #pragma unroll
               for (int w2 = 0; w2 < 8 / (ES / 2); ++w2) {
-                const bool on = bf16_to_f32((uint16_t)(mk[q][w2 >> 1] >> (16 * (w2 & 1)))) > 0.f;
+                const bool on = bf16_to_f32((uint16_t)(mk[g & 1][q][w2 >> 1] >> (16 * (w2 & 1)))) > 0.f;
                 if constexpr (ES == 2) v[q][w2 >> 1] &= on ? 0xffffffffu : (w2 & 1) ? 0xffffu : 0xffff0000u;
                 else v[q][w2] = on ? v[q][w2] : 0u;
               }
@@ -649,10 +646,30 @@ static int launch(const ExpertArgs &a, hipStream_t s) {
   return check_launch("expert_wide");
 }
 
-int run_expert_wide(int pass, const ExpertArgs &a, hipStream_t s) {
+// Tiles of 256 or 128 rows: experts are rarely whole tiles long, and the tiles rarely whole rounds of the CUs, so
+// with few rows an expert the smaller tile wastes less, though it feeds the matrix cores worse (LDS is read for a
+// third more a product). Cycles of a tile: of a slab, and of its start and end (measured); an expert's last tile is
+// taken as half full.
+static int row_tile(const ExpertArgs &a, int tm, int K) {
+  auto cost = [&](int rows, double slab, double ends) {
+    const double tiles = ((double)a.n_rows / rows + 0.5 * (a.n_rows < a.E ? a.n_rows : a.E)) * tm;
+    return std::ceil(tiles / 256.0) * ((K + XW_KS - 1) / XW_KS * slab + ends);
+  };
+  return cost(128, 1350, 11000) < cost(256, 2300, 16000) ? 128 : 256;
+}
+
+template <int PASS>
+static int launch_rows(const ExpertArgs &a, hipStream_t s) {
+  const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in, K = PASS == EXPERT_FWD ? a.d_in : a.d_out;
   const bool half = a.out_dtype == IMBD_BF16;
-  if (pass == EXPERT_FWD) return half ? launch<EXPERT_FWD, 256, 256, 2, 1>(a, s) : launch<EXPERT_FWD, 256, 256, 4, 1>(a, s);
-  if (pass == EXPERT_DX) return half ? launch<EXPERT_DX, 256, 256, 2, 1>(a, s) : launch<EXPERT_DX, 256, 256, 4, 1>(a, s);
+  if (row_tile(a, (M + 255) / 256, K) == 128)
+    return half ? launch<PASS, 256, 128, 2, 1>(a, s) : launch<PASS, 256, 128, 4, 1>(a, s);
+  return half ? launch<PASS, 256, 256, 2, 1>(a, s) : launch<PASS, 256, 256, 4, 1>(a, s);
+}
+
+int run_expert_wide(int pass, const ExpertArgs &a, hipStream_t s) {
+  if (pass == EXPERT_FWD) return launch_rows<EXPERT_FWD>(a, s);
+  if (pass == EXPERT_DX) return launch_rows<EXPERT_DX>(a, s);
   return launch<EXPERT_DW, 256, 256, 4, 1>(a, s);
 }
 
