@@ -83,6 +83,9 @@ int run_expert_tile(int pass, int dtype, const ExpertArgs &a, hipStream_t s);
 // bf16, rows of whole 16-byte chunks (csrc/expert_wide.hip): whether it takes the call, and the launch.
 bool expert_wide_fits(int pass, int dtype, const ExpertArgs &a);
 int run_expert_wide(int pass, const ExpertArgs &a, hipStream_t s);
+// The forward product of few rows an expert (csrc/expert_few.hip).
+bool expert_few_fits(int pass, int dtype, const ExpertArgs &a);
+int run_expert_few(const ExpertArgs &a, hipStream_t s);
 
 size_t route_ws_bytes(int T, int E, int k);
 int run_route(int T, int E, int k, int renorm, const float *logits, int64_t ldl, float *gates, int32_t *experts,

@@ -73,6 +73,7 @@ int check_tensors(const imbd_adamw_tensor *t, int n, size_t *bytes) {
 }
 
 int run_product(int pass, int dtype, const ExpertArgs &a, hipStream_t s) {
+  if (expert_few_fits(pass, dtype, a)) return run_expert_few(a, s);
   return expert_wide_fits(pass, dtype, a) ? run_expert_wide(pass, a, s) : run_expert_tile(pass, dtype, a, s);
 }
 
