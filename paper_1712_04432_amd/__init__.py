@@ -255,23 +255,29 @@ def conv3x3_tile_bwd(x_pad, w, dy_pad, dw, dx=None, ws=None, stream=None):
 # checked by the library (ImbdError).
 def _sizes(t, shape, dtype, name, device, whole=False):
     """Shape, type, device and layout of one tensor: rows without gaps between elements, or
-    (whole) contiguous."""
+    (whole) contiguous. Returns its address."""
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple(shape)}")
     if t.dtype is not dtype:
         raise TypeError(f"{name}: {t.dtype}, need {dtype}")
     if t.device != device:
         raise ValueError(f"{name}: on {t.device}, need {device}")
-    if not t.is_contiguous() and (whole or (t.shape[-1] > 1 and t.stride(-1) != 1)
-                                  or any(s < 0 for s in t.stride())):
+    if not t.is_contiguous() and (whole or (t.shape[-1] > 1 and t.stride(-1) != 1)):
         raise ValueError(f"{name}: strides {t.stride()}")
+    return t.data_ptr()
 
 
 def _here(t, name):
     """The tensor's device, which has to be the current one (the stream is taken from it)."""
-    if not t.is_cuda or t.device.index != _torch().cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, which is not the current device")
-    return t.device
+    dev = t.device
+    if dev.type != "cuda" or dev.index != _torch().cuda.current_device():
+        raise ValueError(f"{name}: on {dev}, which is not the current device")
+    return dev
+
+
+def _on(stream, device):
+    """The address of a stream, or of the device's current one."""
+    return _torch()._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
 def _rows_ld(t):
@@ -282,9 +288,12 @@ def _rows_ld(t):
 
 def _float(t, name):
     torch = _torch()
-    if t.dtype is not torch.bfloat16 and t.dtype is not torch.float32:
-        raise TypeError(f"{name}: {t.dtype}, need torch.bfloat16 or torch.float32")
-    return t.dtype
+    dt = t.dtype
+    if dt is torch.bfloat16:
+        return dt, IMBD_BF16
+    if dt is torch.float32:
+        return dt, IMBD_F32
+    raise TypeError(f"{name}: {dt}, need torch.bfloat16 or torch.float32")
 
 
 def expert_route_workspace_bytes(T: int, E: int, k: int) -> int:
@@ -298,15 +307,13 @@ def expert_route(logits, gates, experts, offsets, rows, slots, ws=None, renorm: 
     T, E = logits.shape
     k = gates.shape[-1]
     i32, f32 = torch.int32, torch.float32
-    _sizes(logits, (T, E), f32, "logits", dev)
-    _sizes(gates, (T, k), f32, "gates", dev, True)
-    _sizes(experts, (T, k), i32, "experts", dev, True)
-    _sizes(offsets, (E + 1,), i32, "offsets", dev, True)
-    _sizes(rows, (T * k,), i32, "rows", dev, True)
-    _sizes(slots, (T, k), i32, "slots", dev, True)
-    check(lib.expert_route(T, E, k, int(bool(renorm)), _ptr(logits), _rows_ld(logits), _ptr(gates), _ptr(experts),
-                           _ptr(offsets), _ptr(rows), _ptr(slots), _ptr(ws),
-                           0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "expert_route")
+    check(lib.expert_route(T, E, k, bool(renorm), _sizes(logits, (T, E), f32, "logits", dev), _rows_ld(logits),
+                           _sizes(gates, (T, k), f32, "gates", dev, True),
+                           _sizes(experts, (T, k), i32, "experts", dev, True),
+                           _sizes(offsets, (E + 1,), i32, "offsets", dev, True),
+                           _sizes(rows, (T * k,), i32, "rows", dev, True),
+                           _sizes(slots, (T, k), i32, "slots", dev, True), None if ws is None else ws.data_ptr(),
+                           0 if ws is None else ws.numel() * ws.element_size(), _on(stream, dev)), "expert_route")
 
 
 def expert_route_bwd(logits, gates, experts, dgates, dlogits, renorm: bool = True, stream=None):
@@ -315,16 +322,13 @@ def expert_route_bwd(logits, gates, experts, dgates, dlogits, renorm: bool = Tru
     lib, dev = load(), _here(dlogits, "dlogits")
     T, E = dlogits.shape
     k = gates.shape[-1]
-    f32 = torch.float32
-    _sizes(dlogits, (T, E), f32, "dlogits", dev)
-    if logits is not None:
-        _sizes(logits, (T, E), f32, "logits", dev)
-    _sizes(gates, (T, k), f32, "gates", dev, True)
-    _sizes(experts, (T, k), torch.int32, "experts", dev, True)
-    _sizes(dgates, (T, k), f32, "dgates", dev, True)
-    check(lib.expert_route_bwd(T, E, k, int(bool(renorm)), _ptr(logits), 0 if logits is None else _rows_ld(logits),
-                               _ptr(gates), _ptr(experts), _ptr(dgates), _ptr(dlogits), _rows_ld(dlogits),
-                               _stream(stream)), "expert_route_bwd")
+    f32, none = torch.float32, logits is None
+    check(lib.expert_route_bwd(T, E, k, bool(renorm), None if none else _sizes(logits, (T, E), f32, "logits", dev),
+                               0 if none else _rows_ld(logits), _sizes(gates, (T, k), f32, "gates", dev, True),
+                               _sizes(experts, (T, k), torch.int32, "experts", dev, True),
+                               _sizes(dgates, (T, k), f32, "dgates", dev, True),
+                               _sizes(dlogits, (T, E), f32, "dlogits", dev), _rows_ld(dlogits), _on(stream, dev)),
+          "expert_route_bwd")
 
 
 def expert_fwd(w, x, offsets, y, bias=None, relu: bool = False, rows=None, stream=None):
@@ -332,19 +336,15 @@ def expert_fwd(w, x, offsets, y, bias=None, relu: bool = False, rows=None, strea
     torch = _torch()
     lib, dev = load(), _here(w, "w")
     E, d_out, d_in = w.shape
-    dt, ydt = _float(w, "w"), _float(y, "y")
-    n, n_x = y.shape[0], x.shape[0]
-    _sizes(w, (E, d_out, d_in), dt, "w", dev)
-    _sizes(x, (n_x, d_in), dt, "x", dev)
-    _sizes(y, (n, d_out), ydt, "y", dev)
-    _sizes(offsets, (E + 1,), torch.int32, "offsets", dev, True)
-    if bias is not None:
-        _sizes(bias, (E, d_out), torch.float32, "bias", dev, True)
-    if rows is not None:
-        _sizes(rows, (n,), torch.int32, "rows", dev, True)
-    check(lib.expert_fwd(dtype_code(dt), int(bool(relu)), E, d_out, d_in, n, n_x, _ptr(w), _rows_ld(w), w.stride(0),
-                         _ptr(bias), _ptr(x), _rows_ld(x), _ptr(rows), _ptr(offsets), _ptr(y), _rows_ld(y),
-                         dtype_code(ydt), _stream(stream)), "expert_fwd")
+    (dt, code), (ydt, ycode) = _float(w, "w"), _float(y, "y")
+    n, n_x, i32 = y.shape[0], x.shape[0], torch.int32
+    check(lib.expert_fwd(code, bool(relu), E, d_out, d_in, n, n_x, _sizes(w, (E, d_out, d_in), dt, "w", dev),
+                         _rows_ld(w), w.stride(0),
+                         None if bias is None else _sizes(bias, (E, d_out), torch.float32, "bias", dev, True),
+                         _sizes(x, (n_x, d_in), dt, "x", dev), _rows_ld(x),
+                         None if rows is None else _sizes(rows, (n,), i32, "rows", dev, True),
+                         _sizes(offsets, (E + 1,), i32, "offsets", dev, True), _sizes(y, (n, d_out), ydt, "y", dev),
+                         _rows_ld(y), ycode, _on(stream, dev)), "expert_fwd")
 
 
 def expert_bwd(w, dy, x, offsets, dw=None, db=None, dx=None, rows=None, mask_relu: bool = False, stream=None):
@@ -353,28 +353,20 @@ def expert_bwd(w, dy, x, offsets, dw=None, db=None, dx=None, rows=None, mask_rel
     torch = _torch()
     lib, dev = load(), _here(w, "w")
     E, d_out, d_in = w.shape
-    dt, n = _float(w, "w"), dy.shape[0]
-    f32 = torch.float32
-    _sizes(w, (E, d_out, d_in), dt, "w", dev)
-    _sizes(dy, (n, d_out), dt, "dy", dev)
-    _sizes(offsets, (E + 1,), torch.int32, "offsets", dev, True)
-    n_x = n
-    if x is not None:
-        n_x = x.shape[0]
-        _sizes(x, (n_x, d_in), dt, "x", dev)
-    if rows is not None:
-        _sizes(rows, (n,), torch.int32, "rows", dev, True)
-    if dw is not None:
-        _sizes(dw, (E, d_out, d_in), f32, "dw", dev)
-    if db is not None:
-        _sizes(db, (E, d_out), f32, "db", dev, True)
-    if dx is not None:
-        _sizes(dx, (n, d_in), _float(dx, "dx"), "dx", dev)
-    check(lib.expert_bwd(dtype_code(dt), E, d_out, d_in, n, n_x, _ptr(w), _rows_ld(w), w.stride(0), _ptr(dy),
-                         _rows_ld(dy), _ptr(x), 0 if x is None else _rows_ld(x), _ptr(rows), _ptr(offsets), _ptr(dw),
-                         0 if dw is None else _rows_ld(dw), 0 if dw is None else dw.stride(0), _ptr(db), _ptr(dx),
-                         0 if dx is None else _rows_ld(dx), IMBD_F32 if dx is None else dtype_code(dx),
-                         int(bool(mask_relu)), _stream(stream)), "expert_bwd")
+    dt, code = _float(w, "w")
+    n, f32, i32 = dy.shape[0], torch.float32, torch.int32
+    n_x = n if x is None else x.shape[0]
+    dxdt, dxcode = (None, IMBD_F32) if dx is None else _float(dx, "dx")
+    check(lib.expert_bwd(code, E, d_out, d_in, n, n_x, _sizes(w, (E, d_out, d_in), dt, "w", dev), _rows_ld(w),
+                         w.stride(0), _sizes(dy, (n, d_out), dt, "dy", dev), _rows_ld(dy),
+                         None if x is None else _sizes(x, (n_x, d_in), dt, "x", dev), 0 if x is None else _rows_ld(x),
+                         None if rows is None else _sizes(rows, (n,), i32, "rows", dev, True),
+                         _sizes(offsets, (E + 1,), i32, "offsets", dev, True),
+                         None if dw is None else _sizes(dw, (E, d_out, d_in), f32, "dw", dev),
+                         0 if dw is None else _rows_ld(dw), 0 if dw is None else dw.stride(0),
+                         None if db is None else _sizes(db, (E, d_out), f32, "db", dev, True),
+                         None if dx is None else _sizes(dx, (n, d_in), dxdt, "dx", dev),
+                         0 if dx is None else _rows_ld(dx), dxcode, bool(mask_relu), _on(stream, dev)), "expert_bwd")
 
 
 def expert_combine(ys, slots, y, gates=None, stream=None):
@@ -383,14 +375,12 @@ def expert_combine(ys, slots, y, gates=None, stream=None):
     lib, dev = load(), _here(ys, "ys")
     n, d = ys.shape
     T, k = slots.shape
-    dt, ydt = _float(ys, "ys"), _float(y, "y")
-    _sizes(ys, (n, d), dt, "ys", dev)
-    _sizes(y, (T, d), ydt, "y", dev)
-    _sizes(slots, (T, k), torch.int32, "slots", dev, True)
-    if gates is not None:
-        _sizes(gates, (T, k), torch.float32, "gates", dev, True)
-    check(lib.expert_combine(dtype_code(dt), T, k, d, n, _ptr(ys), _rows_ld(ys), _ptr(slots), _ptr(gates), _ptr(y),
-                             _rows_ld(y), dtype_code(ydt), _stream(stream)), "expert_combine")
+    (dt, code), (ydt, ycode) = _float(ys, "ys"), _float(y, "y")
+    check(lib.expert_combine(code, T, k, d, n, _sizes(ys, (n, d), dt, "ys", dev), _rows_ld(ys),
+                             _sizes(slots, (T, k), torch.int32, "slots", dev, True),
+                             None if gates is None else _sizes(gates, (T, k), torch.float32, "gates", dev, True),
+                             _sizes(y, (T, d), ydt, "y", dev), _rows_ld(y), ycode, _on(stream, dev)),
+          "expert_combine")
 
 
 def expert_combine_bwd(dy, ys, slots, gates, dys, dgates=None, stream=None):
@@ -400,18 +390,15 @@ def expert_combine_bwd(dy, ys, slots, gates, dys, dgates=None, stream=None):
     lib, dev = load(), _here(dy, "dy")
     T, d = dy.shape
     n, k = dys.shape[0], slots.shape[-1]
-    dt = _float(dy, "dy")
-    _sizes(dy, (T, d), dt, "dy", dev)
-    _sizes(dys, (n, d), dt, "dys", dev)
-    if ys is not None:
-        _sizes(ys, (n, d), dt, "ys", dev)
-    _sizes(slots, (T, k), torch.int32, "slots", dev, True)
-    _sizes(gates, (T, k), torch.float32, "gates", dev, True)
-    if dgates is not None:
-        _sizes(dgates, (T, k), torch.float32, "dgates", dev, True)
-    check(lib.expert_combine_bwd(dtype_code(dt), T, k, d, n, _ptr(dy), _rows_ld(dy), _ptr(ys),
-                                 0 if ys is None else _rows_ld(ys), _ptr(slots), _ptr(gates), _ptr(dys), _rows_ld(dys),
-                                 _ptr(dgates), _stream(stream)), "expert_combine_bwd")
+    dt, code = _float(dy, "dy")
+    f32 = torch.float32
+    check(lib.expert_combine_bwd(code, T, k, d, n, _sizes(dy, (T, d), dt, "dy", dev), _rows_ld(dy),
+                                 None if ys is None else _sizes(ys, (n, d), dt, "ys", dev),
+                                 0 if ys is None else _rows_ld(ys),
+                                 _sizes(slots, (T, k), torch.int32, "slots", dev, True),
+                                 _sizes(gates, (T, k), f32, "gates", dev, True), _sizes(dys, (n, d), dt, "dys", dev),
+                                 _rows_ld(dys), None if dgates is None else _sizes(dgates, (T, k), f32, "dgates", dev, True),
+                                 _on(stream, dev)), "expert_combine_bwd")
 
 
 # ------------------------------------------------------------------------------- AdamW
@@ -436,7 +423,7 @@ class AdamW:
             w, n = t["w"], t["w"].numel()
             bits8 = t["m"].dtype is torch.float8_e4m3fn
             _sizes(w, w.shape, f32, "w", dev, True)
-            _sizes(t["grad"], w.shape, _float(t["grad"], "grad"), "grad", dev, True)
+            _sizes(t["grad"], w.shape, _float(t["grad"], "grad")[0], "grad", dev, True)
             _sizes(t["m"], w.shape, torch.float8_e4m3fn if bits8 else f32, "m", dev, True)
             _sizes(t["v"], w.shape, torch.float8_e5m2 if bits8 else f32, "v", dev, True)
             if t.get("w_lp") is not None:
@@ -457,23 +444,25 @@ class AdamW:
         # (a plan of no bytes: nothing to update, or a bad argument, which this call reports)
         check(lib.adamw_plan(arr, len(tensors), _ptr(host), self.bytes), "adamw_plan")
         self.plan = host.to(dev)
+        self.address = self.plan.data_ptr()
 
 
 def adamw_step(plan: AdamW, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step=1,
                grad_scale: float = 1.0, stream=None):
     """One AdamW step on every tensor of a plan. step: the step's number, from 1 on, or a device int32
     tensor that holds it (read by the kernel, so a captured launch follows it)."""
-    lib = load()
-    if plan.device.index != _torch().cuda.current_device():
-        raise ValueError(f"plan: on {plan.device}, which is not the current device")
+    lib, torch = load(), _torch()
+    dev = plan.device
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"plan: on {dev}, which is not the current device")
     dev_step = None
     if not isinstance(step, int):
-        _sizes(step, step.shape, _torch().int32, "step", plan.device, True)
+        dev_step = _sizes(step, step.shape, torch.int32, "step", dev, True)
         if step.numel() != 1:
             raise ValueError(f"step: {step.numel()} elements, need 1")
-        dev_step, step = _ptr(step), 1
-    check(lib.adamw_step(_ptr(plan.plan), plan.bytes, plan.n_tensors, float(lr), float(beta1), float(beta2),
-                         float(eps), float(grad_scale), step, dev_step, _stream(stream)), "adamw_step")
+        step = 1
+    check(lib.adamw_step(plan.address, plan.bytes, plan.n_tensors, lr, beta1, beta2, eps, grad_scale, step, dev_step,
+                         _on(stream, dev)), "adamw_step")
 
 
 def timing_begin(kernel_class: int, layer: int = -1, max_launches: int = 1000):
