@@ -38,7 +38,7 @@ struct AwTensor {
   float decay;
   int32_t flags;
 };
-enum { AW_GRAD_BF16 = 1, AW_STATE8 = 2, AW_VECTOR = 4 };
+enum { AW_GRAD_BF16 = 1, AW_STATE8 = 2, AW_VECTOR = 4, AW_STREAM = 8 };
 struct AwEntry {
   uint32_t tensor, chunk;
 };
@@ -106,32 +106,40 @@ __device__ __forceinline__ float advance(const Step &st, float w, float g, float
   return w0 - d;
 }
 
-// Four elements i .. i+3 of one tensor, n of them real (4 in the vector form).
-template <bool VEC, typename T>
+// Four elements of one tensor: n of them real, one by one; whole vectors; whole vectors past the caches.
+enum { AW_ONES = 0, AW_WHOLE = 1, AW_PAST = 2 };
+template <int HOW, typename T>
 __device__ __forceinline__ void load4(const T *p, int n, T (&v)[4]) {
-  if constexpr (VEC) {
-    __builtin_memcpy(v, __builtin_assume_aligned(p, 4 * sizeof(T)), 4 * sizeof(T));
-  } else {
+  if constexpr (HOW == AW_ONES) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = e < n ? p[e] : T(0);
+  } else {
+    typedef T V __attribute__((ext_vector_type(4)));
+    const V x = HOW == AW_PAST ? __builtin_nontemporal_load(reinterpret_cast<const V *>(p)) : *reinterpret_cast<const V *>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = x[e];
   }
 }
-template <bool VEC, typename T>
+template <int HOW, typename T>
 __device__ __forceinline__ void store4(T *p, int n, const T (&v)[4]) {
-  if constexpr (VEC) {
-    __builtin_memcpy(__builtin_assume_aligned(p, 4 * sizeof(T)), v, 4 * sizeof(T));
-  } else {
+  if constexpr (HOW == AW_ONES) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (e < n) p[e] = v[e];
+  } else {
+    typedef T V __attribute__((ext_vector_type(4)));
+    const V x = {v[0], v[1], v[2], v[3]};
+    if constexpr (HOW == AW_PAST) __builtin_nontemporal_store(x, reinterpret_cast<V *>(p));
+    else *reinterpret_cast<V *>(p) = x;
   }
 }
 
-// A chunk: wave `wave` takes blocks wave, wave + 4, .. of 256 elements. VEC: whole blocks at 16-byte
-// aligned addresses; else element by element, with the tensor's end inside.
-template <bool VEC, bool G16, bool S8>
+// A chunk: wave `wave` takes blocks wave, wave + 4, .. of 256 elements. AW_ONES: element by element, with the
+// tensor's end inside; else whole blocks at 16-byte aligned addresses.
+template <int HOW, bool G16, bool S8>
 __device__ __forceinline__ void chunk(const AwTensor &a, const Step &st, int64_t start) {
   constexpr int NB = AW_CHUNK / AW_BLOCK / (AW_NT / 64);  // blocks a wave
+  constexpr bool VEC = HOW != AW_ONES;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float w[NB][4], m[NB][4], v[NB][4], g[NB][4], ms[NB], vs[NB];
   int n[NB];
@@ -140,19 +148,19 @@ __device__ __forceinline__ void chunk(const AwTensor &a, const Step &st, int64_t
     const int64_t blk = start / AW_BLOCK + wave + b * (AW_NT / 64), i = blk * AW_BLOCK + 4 * lane;
     const int64_t left = a.n - i;
     n[b] = VEC ? 4 : (int)min((int64_t)4, max((int64_t)0, left));
-    load4<VEC>(a.w + i, n[b], w[b]);
+    load4<HOW>(a.w + i, n[b], w[b]);
     if constexpr (G16) {
       uint16_t h[4];
-      load4<VEC>(reinterpret_cast<const uint16_t *>(a.grad) + i, n[b], h);
+      load4<HOW>(reinterpret_cast<const uint16_t *>(a.grad) + i, n[b], h);
 #pragma unroll
       for (int e = 0; e < 4; ++e) g[b][e] = bf16_to_f32(h[e]);
     } else {
-      load4<VEC>(reinterpret_cast<const float *>(a.grad) + i, n[b], g[b]);
+      load4<HOW>(reinterpret_cast<const float *>(a.grad) + i, n[b], g[b]);
     }
     if constexpr (S8) {
       uint8_t mc[4], vc[4];
-      load4<VEC>(reinterpret_cast<const uint8_t *>(a.m) + i, n[b], mc);
-      load4<VEC>(reinterpret_cast<const uint8_t *>(a.v) + i, n[b], vc);
+      load4<HOW>(reinterpret_cast<const uint8_t *>(a.m) + i, n[b], mc);
+      load4<HOW>(reinterpret_cast<const uint8_t *>(a.v) + i, n[b], vc);
       const bool real = VEC || blk * AW_BLOCK < a.n;
       ms[b] = real ? a.m_scale[blk] : 0.f;
       vs[b] = real ? a.v_scale[blk] : 0.f;
@@ -168,8 +176,8 @@ __device__ __forceinline__ void chunk(const AwTensor &a, const Step &st, int64_t
         v[b][e] = value_e5m2(vc[e]) * vs[b];
       }
     } else {
-      load4<VEC>(reinterpret_cast<const float *>(a.m) + i, n[b], m[b]);
-      load4<VEC>(reinterpret_cast<const float *>(a.v) + i, n[b], v[b]);
+      load4<HOW>(reinterpret_cast<const float *>(a.m) + i, n[b], m[b]);
+      load4<HOW>(reinterpret_cast<const float *>(a.v) + i, n[b], v[b]);
     }
   }
 #pragma unroll
@@ -178,11 +186,11 @@ __device__ __forceinline__ void chunk(const AwTensor &a, const Step &st, int64_t
     if (!VEC && blk * AW_BLOCK >= a.n) continue;  // (the whole wave)
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[b][e] = advance(st, w[b][e], g[b][e], m[b][e], v[b][e]);
-    store4<VEC>(a.w + i, n[b], w[b]);
+    store4<HOW>(a.w + i, n[b], w[b]);
     if (a.w_lp) {
       const uint32_t lo = cvt_pk_bf16(w[b][0], w[b][1]), hi = cvt_pk_bf16(w[b][2], w[b][3]);
       const uint16_t h[4] = {(uint16_t)lo, (uint16_t)(lo >> 16), (uint16_t)hi, (uint16_t)(hi >> 16)};
-      store4<VEC>(a.w_lp + i, n[b], h);
+      store4<HOW>(a.w_lp + i, n[b], h);
     }
     if constexpr (S8) {
       // (elements past the tensor's end are zero: they do not raise a maximum)
@@ -209,11 +217,11 @@ __device__ __forceinline__ void chunk(const AwTensor &a, const Step &st, int64_t
       uint32_t mq = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
       mq = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], mq, true);
       __builtin_memcpy(mc, &mq, 4);
-      store4<VEC>(reinterpret_cast<uint8_t *>(a.m) + i, n[b], mc);
-      store4<VEC>(reinterpret_cast<uint8_t *>(a.v) + i, n[b], vc);
+      store4<HOW>(reinterpret_cast<uint8_t *>(a.m) + i, n[b], mc);
+      store4<HOW>(reinterpret_cast<uint8_t *>(a.v) + i, n[b], vc);
     } else {
-      store4<VEC>(reinterpret_cast<float *>(a.m) + i, n[b], m[b]);
-      store4<VEC>(reinterpret_cast<float *>(a.v) + i, n[b], v[b]);
+      store4<HOW>(reinterpret_cast<float *>(a.m) + i, n[b], m[b]);
+      store4<HOW>(reinterpret_cast<float *>(a.v) + i, n[b], v[b]);
     }
   }
 }
@@ -235,15 +243,20 @@ __global__ void __launch_bounds__(AW_NT) adamw_kernel(AwArgs a) {
   st.t = (uint32_t)step;
   const int64_t start = (int64_t)en.chunk * AW_CHUNK;
   const bool whole = (t.flags & AW_VECTOR) && start + AW_CHUNK <= t.n;
-  switch ((whole ? 4 : 0) | (t.flags & (AW_GRAD_BF16 | AW_STATE8))) {
-    case 0: chunk<false, false, false>(t, st, start); break;
-    case 1: chunk<false, true, false>(t, st, start); break;
-    case 2: chunk<false, false, true>(t, st, start); break;
-    case 3: chunk<false, true, true>(t, st, start); break;
-    case 4: chunk<true, false, false>(t, st, start); break;
-    case 5: chunk<true, true, false>(t, st, start); break;
-    case 6: chunk<true, false, true>(t, st, start); break;
-    default: chunk<true, true, true>(t, st, start); break;
+  const int how = !whole ? AW_ONES : (t.flags & AW_STREAM) ? AW_PAST : AW_WHOLE;
+  switch (how * 4 + (t.flags & (AW_GRAD_BF16 | AW_STATE8))) {
+    case 0: chunk<AW_ONES, false, false>(t, st, start); break;
+    case 1: chunk<AW_ONES, true, false>(t, st, start); break;
+    case 2: chunk<AW_ONES, false, true>(t, st, start); break;
+    case 3: chunk<AW_ONES, true, true>(t, st, start); break;
+    case 4: chunk<AW_WHOLE, false, false>(t, st, start); break;
+    case 5: chunk<AW_WHOLE, true, false>(t, st, start); break;
+    case 6: chunk<AW_WHOLE, false, true>(t, st, start); break;
+    case 7: chunk<AW_WHOLE, true, true>(t, st, start); break;
+    case 8: chunk<AW_PAST, false, false>(t, st, start); break;
+    case 9: chunk<AW_PAST, true, false>(t, st, start); break;
+    case 10: chunk<AW_PAST, false, true>(t, st, start); break;
+    default: chunk<AW_PAST, true, true>(t, st, start); break;
   }
 }
 
@@ -254,6 +267,14 @@ size_t adamw_record_bytes() { return sizeof(AwTensor); }
 size_t adamw_entry_bytes() { return sizeof(AwEntry); }
 
 void adamw_write_plan(const imbd_adamw_tensor *tensors, int n_tensors, void *plan) {
+  // What the set reads and writes in a step. Up to twice the 256 MB of the memory-side cache part of it is still
+  // there a step later; past that the loads and stores go past the caches (fp32 state: 16M elements, 448 MB, 74 us,
+  // and 81 past the caches; 64M, 1.8 GB, 353 and 326. 8-bit state: 16M, 192 MB, 52 and 55; 64M, 770 MB, 226 and 211).
+  int64_t bytes = 0;
+  for (int i = 0; i < n_tensors; ++i)
+    bytes += tensors[i].n * (4 + (tensors[i].w_lp ? 2 : 0) + (tensors[i].grad_dtype == IMBD_BF16 ? 2 : 4) +
+                             (tensors[i].state_bits == 8 ? 2 : 8));
+  const bool stream = bytes > (int64_t)512 << 20;
   AwTensor *rec = reinterpret_cast<AwTensor *>(plan);
   AwEntry *en = reinterpret_cast<AwEntry *>(rec + n_tensors);
   for (int i = 0; i < n_tensors; ++i) {
@@ -263,7 +284,7 @@ void adamw_write_plan(const imbd_adamw_tensor *tensors, int n_tensors, void *pla
     const uintptr_t sa = s8 ? 4 : 16;
     const bool vec = al(t.w, 16) && al(t.w_lp, 8) && al(t.grad, g16 ? 8 : 16) && al(t.m, sa) && al(t.v, sa);
     rec[i] = AwTensor{t.w, t.w_lp, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.n, t.decay,
-                      (g16 ? AW_GRAD_BF16 : 0) | (s8 ? AW_STATE8 : 0) | (vec ? AW_VECTOR : 0)};
+                      (g16 ? AW_GRAD_BF16 : 0) | (s8 ? AW_STATE8 : 0) | (vec ? AW_VECTOR : 0) | (stream ? AW_STREAM : 0)};
     const int64_t c = adamw_chunks(t.n);
     for (int64_t j = 0; j < c; ++j) *en++ = AwEntry{(uint32_t)i, (uint32_t)j};
   }

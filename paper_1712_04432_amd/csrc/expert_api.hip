@@ -177,6 +177,7 @@ int expert_bwd(int dtype, int E, int d_out, int d_in, int n_rows, int n_x, const
   if (!dw && !db) return IMBD_OK;
   a.mask = 0;
   a.x = x;
+  if (!dw) a.n_x = 0;  // (db alone: x may be NULL and is not read)
   a.out = dw; a.ldo = lddw; a.so = sdw; a.out_dtype = IMBD_F32;
   a.db = db;
   return run_product(EXPERT_DW, dtype, a, stream_of(stream));

@@ -2,7 +2,8 @@
 //   y[t]       = sum_j g[t][j] ys[slot[t][j]]
 //   dys[slot]  = g[t][j] dy[t],   dg[t][j] = dy[t] . ys[slot[t][j]]
 // Both are streams: every row of ys is read (and of dys written) once, in whole 16-byte chunks where base
-// and pitch allow, 0.5 flop a byte.
+// and pitch allow, 0.5 flop a byte. Outputs are stored past the caches (nothing here reads them again; 16384
+// tokens, k = 2, 4096 columns of bf16: 80 -> 59 us, backward 148 -> 130 us; reading past them too, 72 and 165).
 
 #include "expert.h"
 
@@ -50,11 +51,11 @@ __device__ __forceinline__ void store_f32(T *p, const float (&v)[VEC]) {
     u32x4 q;
 #pragma unroll
     for (int e = 0; e < 4; ++e) q[e] = cvt_pk_bf16(v[2 * e], v[2 * e + 1]);
-    *reinterpret_cast<u32x4 *>(p) = q;
+    __builtin_nontemporal_store(q, reinterpret_cast<u32x4 *>(p));
   } else {
 #pragma unroll
     for (int h = 0; h < VEC / 4; ++h)
-      reinterpret_cast<f32x4 *>(p)[h] = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+      __builtin_nontemporal_store(f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]}, reinterpret_cast<f32x4 *>(p) + h);
   }
 }
 

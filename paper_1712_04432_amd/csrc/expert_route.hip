@@ -34,23 +34,42 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 }
 constexpr uint32_t KEY_MINUS_INF = 0x007fffffu;  // order_key(-inf)
 
-template <int G>
+// The value of the lane that a group's reduction pairs with at distance o: inside 16 lanes by the cross-lane forms
+// of the vector instructions (at 4 and 8 the mirrored lane, which holds the same as its neighbours by then).
+template <int o>
+__device__ __forceinline__ int partner(int v) {
+  if constexpr (o == 1) return __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, false);        // quad: 1 0 3 2
+  else if constexpr (o == 2) return __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, false);   // quad: 2 3 0 1
+  else if constexpr (o == 4) return __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, false);  // half rows mirrored
+  else if constexpr (o == 8) return __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, false);  // rows mirrored
+  else return __shfl_xor(v, o, 64);
+}
+template <int G, int o = 1>
 __device__ __forceinline__ uint32_t group_max(uint32_t v) {
-#pragma unroll
-  for (int o = 1; o < G; o <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-  return v;
+  if constexpr (o >= G) return v;
+  else return group_max<G, 2 * o>(max(v, (uint32_t)partner<o>((int)v)));
 }
-template <int G>
+template <int G, int o = 1>
 __device__ __forceinline__ int group_min(int v) {
-#pragma unroll
-  for (int o = 1; o < G; o <<= 1) v = min(v, __shfl_xor(v, o, 64));
-  return v;
+  if constexpr (o >= G) return v;
+  else return group_min<G, 2 * o>(min(v, partner<o>(v)));
 }
-template <int G>
+template <int G, int o = 1>
 __device__ __forceinline__ float group_sum(float v) {
+  if constexpr (o >= G) return v;
+  else return group_sum<G, 2 * o>(v + __builtin_bit_cast(float, partner<o>(__builtin_bit_cast(int, v))));
+}
+
+// Eight consecutive values from p (n of them real, the others `none`).
+__device__ __forceinline__ void load8(const float *p, int n, float none, float (&v)[8]) {
+  if (n >= 8) {
+    const f32x4 a = *reinterpret_cast<const f32x4_any *>(p), b = *reinterpret_cast<const f32x4_any *>(p + 4);
 #pragma unroll
-  for (int o = 1; o < G; o <<= 1) v += __shfl_xor(v, o, 64);
-  return v;
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : none;
+  }
 }
 
 struct RouteArgs {
@@ -70,10 +89,11 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int t, int q, F count
   constexpr int VPL = 8;
   const float *z = a.logits + (int64_t)t * a.ldl;
   uint32_t key[VPL];
+  float zv[VPL];
+  load8(z + q * VPL, a.E - q * VPL, -INFINITY, zv);
 #pragma unroll
   for (int i = 0; i < VPL; ++i) {
-    const int e = q * VPL + i;
-    const uint32_t u = e < a.E ? order_key(z[e]) : 0u;
+    const uint32_t u = order_key(zv[i]);
     key[i] = u == KEY_MINUS_INF ? 0u : u;  // never chosen
   }
   float all = 0.f, peak = 0.f;
@@ -244,60 +264,66 @@ struct RouteBwdArgs {
   int64_t lddl;
 };
 
-// G lanes a token, as in the choice; the k pairs are read by every lane of the group (one cached line).
-template <int G>
+// G lanes a token, as in the choice; the k <= KM pairs are read by every lane of the group (the same cached lines),
+// all at once.
+template <int G, int KM>
 __global__ void __launch_bounds__(256) route_bwd_kernel(RouteBwdArgs a) {
   constexpr int VPL = 8;
   const int q = threadIdx.x % G, t = blockIdx.x * (256 / G) + threadIdx.x / G;
   if (t >= a.T) return;  // (whole groups)
   const int64_t p0 = (int64_t)t * a.k;
-  float dz[VPL];
+  int e[KM];
+  float g[KM], dg[KM], v[VPL];
+#pragma unroll
+  for (int j = 0; j < KM; ++j) {
+    const bool in = j < a.k;
+    e[j] = in ? a.experts[p0 + j] : -1;
+    g[j] = in ? a.gates[p0 + j] : 0.f;
+    dg[j] = in ? a.dgates[p0 + j] : 0.f;
+  }
+  if (!a.renorm) load8(a.logits + (int64_t)t * a.ldl + q * VPL, a.E - q * VPL, -INFINITY, v);
+  float dz[VPL], inner = 0.f;
 #pragma unroll
   for (int i = 0; i < VPL; ++i) dz[i] = 0.f;
-  float inner = 0.f;
-  for (int j = 0; j < a.k; ++j)
-    if (a.experts[p0 + j] >= 0) inner = fmaf(a.gates[p0 + j], a.dgates[p0 + j], inner);
-  const float off = a.renorm ? inner : 0.f;
-  for (int j = 0; j < a.k; ++j) {
-    const int at = a.experts[p0 + j] - q * VPL;
-    const float v = a.gates[p0 + j] * (a.dgates[p0 + j] - off);
 #pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      if (at == i) dz[i] += v;
+  for (int j = 0; j < KM; ++j)
+    if (e[j] >= 0) inner = fmaf(g[j], dg[j], inner);
+  const float off = a.renorm ? inner : 0.f;
+#pragma unroll
+  for (int j = 0; j < KM; ++j) {
+    const int at = e[j] - q * VPL;
+    const float add = g[j] * (dg[j] - off);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) dz[i] += e[j] >= 0 && at == i ? add : 0.f;
   }
   if (!a.renorm) {
-    const float *z = a.logits + (int64_t)t * a.ldl;
-    float v[VPL], peak = -INFINITY, sum = 0.f;
-    bool nan = false;
+    uint32_t top = 0u;  // (as whole numbers of the same order: a NaN counts)
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      const int e = q * VPL + i;
-      v[i] = e < a.E ? z[e] : -INFINITY;
-      peak = fmaxf(peak, v[i]);
-      nan |= v[i] != v[i];
-    }
-#pragma unroll
-    for (int o = 1; o < G; o <<= 1) peak = fmaxf(peak, __shfl_xor(peak, o, 64));
-    if (peak > -INFINITY || nan) {
+    for (int i = 0; i < VPL; ++i) top = max(top, order_key(v[i]));
+    top = group_max<G>(top);
+    if (top > KEY_MINUS_INF) {
+      const float peak = key_value(top);
+      float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < VPL; ++i) {
         v[i] = v[i] == -INFINITY ? 0.f : expf(v[i] - peak);
         sum += v[i];
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) v[i] = 0.f;
-    }
-    sum = group_sum<G>(sum);
-    if (sum != 0.f) {
+      sum = group_sum<G>(sum);
 #pragma unroll
       for (int i = 0; i < VPL; ++i) dz[i] -= v[i] / sum * inner;
     }
   }
-  float *out = a.dlogits + (int64_t)t * a.lddl;
+  float *out = a.dlogits + (int64_t)t * a.lddl + q * VPL;
+  const int n = a.E - q * VPL;
+  if (n >= VPL) {
+    *reinterpret_cast<f32x4_any *>(out) = f32x4{dz[0], dz[1], dz[2], dz[3]};
+    *reinterpret_cast<f32x4_any *>(out + 4) = f32x4{dz[4], dz[5], dz[6], dz[7]};
+  } else {
 #pragma unroll
-  for (int i = 0; i < VPL; ++i)
-    if (q * VPL + i < a.E) out[q * VPL + i] = dz[i];
+    for (int i = 0; i < VPL; ++i)
+      if (i < n) out[i] = dz[i];
+  }
 }
 
 // Tokens of a workgroup, and the number of workgroups.
@@ -362,10 +388,16 @@ int run_route_bwd(int T, int E, int k, int renorm, const float *logits, int64_t 
   const dim3 grid((unsigned)(((int64_t)T + per - 1) / per)), wg(256);
   {
     LaunchTimer t(IMBD_K_ROUTE, 2, s);
-    if (G == 8) hipLaunchKernelGGL(route_bwd_kernel<8>, grid, wg, 0, s, a);
-    else if (G == 16) hipLaunchKernelGGL(route_bwd_kernel<16>, grid, wg, 0, s, a);
-    else if (G == 32) hipLaunchKernelGGL(route_bwd_kernel<32>, grid, wg, 0, s, a);
-    else hipLaunchKernelGGL(route_bwd_kernel<64>, grid, wg, 0, s, a);
+#define GO(G_)                                                                           \
+  do {                                                                                   \
+    if (k <= 8) hipLaunchKernelGGL((route_bwd_kernel<G_, 8>), grid, wg, 0, s, a);        \
+    else hipLaunchKernelGGL((route_bwd_kernel<G_, CHOICE_MAX>), grid, wg, 0, s, a);      \
+  } while (0)
+    if (G == 8) GO(8);
+    else if (G == 16) GO(16);
+    else if (G == 32) GO(32);
+    else GO(64);
+#undef GO
   }
   return check_launch("expert_route_bwd");
 }

@@ -218,6 +218,7 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     } else if constexpr (PASS == EXPERT_DX) {
       return k_rows(w + m0, a.ldw, M - m0);
     } else if constexpr (!GATHER) {
+      if (a.n_x == 0) return Window(nullptr, 0, 0u, 0u);  // (no x: db alone)
       return k_rows(x + (int64_t)r0 * a.ldx + m0, a.ldx, M - m0);
     } else {  // any row of x: the k-rows that do not exist are masked by lane
       const uint32_t n = a.n_x > 0 ? (uint32_t)(((int64_t)(a.n_x - 1) * a.ldx + M - m0) * 2) : 0u;

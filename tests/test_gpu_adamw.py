@@ -259,6 +259,26 @@ def test_same_bits_again_and_beside_others(imbd, dev):
                     assert torch.equal(x[k].view(torch.uint8), y[k].view(torch.uint8))
 
 
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+def test_same_bits_in_a_set_past_the_caches(imbd, dev, grad):
+    """A set of more than 512 MB reads and writes past the caches: the bits stay."""
+    import torch
+    n = 20_000_000
+    z = lambda: torch.zeros(n, device=dev)  # noqa: E731
+    big = {"w": z(), "w_lp": z().to(torch.bfloat16), "grad": z(), "m": z(), "v": z()}
+    for bits in (32, 8):
+        pairs = _tensors(dev, SIZES, bits, grad, seed=8)
+        alone = [t for t, _ in _tensors(dev, SIZES, bits, grad, seed=8)]
+        imbd.adamw_step(imbd.AdamW([big] + [t for t, _ in pairs]), step=5, **HYPER)
+        imbd.adamw_step(imbd.AdamW(alone), step=5, **HYPER)
+        torch.cuda.synchronize()
+        for (x, whole), y in zip(pairs, alone):
+            for k in x:
+                if k != "decay":
+                    assert torch.equal(x[k].view(torch.uint8), y[k].view(torch.uint8)), k
+    assert not big["w"].any() and not big["v"].any()
+
+
 def test_refusals(imbd, dev):
     import torch
     (t, _), = _tensors(dev, [512], 32, "f32", 9)

@@ -163,6 +163,77 @@ def test_products_bf16_layers(imbd, dev, counts, d_out, d_in, pad, gather):
     _check_bwd(imbd, L, mask=True)
 
 
+@pytest.mark.parametrize("wide,K", [(3832, 72), (3840, 200), (3832, 328), (3840, 64), (3832, 8)])
+@pytest.mark.parametrize("counts", [[2500, 1600], [1, 4090, 9]])
+@pytest.mark.parametrize("gather,out", [(False, "bf16"), (True, "bf16"), (True, "f32")])
+def test_products_on_tiles_of_256_rows(imbd, dev, wide, K, counts, gather, out):
+    """Sizes whose tiles of 256 rows are one round of the CUs and those of 128 two, which is where the larger tile is
+    taken; K from less than one slab to several, even and odd numbers of them, whole and cut."""
+    L = Layer(dev, counts, wide, K, "bf16", gather=gather, spare=2, pad=8, seed=K)
+    _check_fwd(imbd, L, relu=gather, out=out)
+    L = Layer(dev, counts, K, wide, "bf16", gather=gather, spare=2, pad=8, seed=K)
+    _check_bwd(imbd, L, mask=True, out=out)
+
+
+@pytest.mark.parametrize("dtype,d_out,d_in", [("bf16", 256, 512), ("bf16", 264, 99), ("f32", 66, 70)])
+@pytest.mark.parametrize("gather", [False, True])
+def test_bias_gradient_without_x(imbd, dev, dtype, d_out, d_in, gather):
+    """db alone needs no x; dw of slots whose rows do not exist (an x of no rows) is zero."""
+    import torch
+    L = Layer(dev, [5, 0, 130, 300], d_out, d_in, dtype, gather=gather, seed=4)
+    want = _check_bwd(imbd, L, which="db")[1]
+    db = torch.full((L.E, d_out), 7.0, device=dev)
+    imbd.expert_bwd(L.w, L.dy, None, L.offsets, db=db, rows=L.rows)
+    assert torch.equal(db, want)
+    if gather:
+        dw = torch.full((L.E, d_out, d_in), 7.0, device=dev)
+        imbd.expert_bwd(L.w, L.dy, L.x[:0], L.offsets, dw=dw, db=db, rows=L.rows)
+        assert not dw.any() and torch.equal(db, want)
+    # dx alone without a mask needs no x either
+    dx, ref = (torch.zeros(L.n, d_in, dtype=L.dt, device=dev) for _ in range(2))
+    imbd.expert_bwd(L.w, L.dy, None, L.offsets, dx=dx)
+    imbd.expert_bwd(L.w, L.dy, L.x, L.offsets, dx=ref, rows=L.rows)
+    assert torch.equal(dx, ref)
+
+
+def test_long_rows_and_many_slots(imbd, dev):
+    """Offsets past 32 bits of bytes in every operand: x gathered from the end of more than 4 GiB (the kernel for any
+    size), rows in expert order past 4 GiB (the large tiles, whose windows move), and their gradients."""
+    import torch
+    n_x, d = 70000, 32768  # 4.6 GB of bf16
+    big = torch.zeros(n_x, d, dtype=torch.bfloat16, device=dev)
+    g = _gen(1, dev)
+    big[-3:] = torch.randn(3, d, generator=g, device=dev)
+    w = (torch.randn(2, 64, d, generator=g, device=dev) * d ** -0.5).to(torch.bfloat16)
+    bias = torch.randn(2, 64, generator=g, device=dev)
+    rows = torch.tensor([n_x - 1, n_x - 3, 5, n_x - 2] * 30, dtype=torch.int32, device=dev)
+    off = torch.tensor([0, 50, 120], dtype=torch.int32, device=dev)
+    y = torch.zeros(120, 64, device=dev)
+    imbd.expert_fwd(w, big, off, y, bias=bias, rows=rows)
+    for e, s in ((0, slice(0, 50)), (1, slice(50, 120))):
+        x = big[rows[s].long()].double()
+        _close(y[s], x @ w[e].double().t() + bias[e].double(), x.abs() @ w[e].double().abs().t() + bias[e].double().abs(),
+               d + 1, "f32", "gathered")
+    # in expert order: the last expert owns the last rows
+    off = torch.tensor([0, n_x - 3, n_x], dtype=torch.int32, device=dev)
+    y = torch.zeros(n_x, 64, dtype=torch.bfloat16, device=dev)
+    imbd.expert_fwd(w, big, off, y, bias=bias)
+    x = big[-3:].double()
+    _close(y[-3:], x @ w[1].double().t() + bias[1].double(), x.abs() @ w[1].double().abs().t() + bias[1].double().abs(), d + 1,
+           "bf16", "in order")
+    assert torch.equal(y[:-3], bias[0].to(torch.bfloat16).expand(n_x - 3, 64))
+    dy = torch.zeros(n_x, 64, dtype=torch.bfloat16, device=dev)
+    dy[-3:] = torch.randn(3, 64, generator=g, device=dev)
+    dw, db = torch.empty(2, 64, d, device=dev), torch.empty(2, 64, device=dev)
+    dx = torch.full((n_x, d), 3.0, dtype=torch.bfloat16, device=dev)
+    imbd.expert_bwd(w, dy, big, off, dw=dw, db=db, dx=dx)
+    c = dy[-3:].double()
+    _close(dw[1], c.t() @ x, c.abs().t() @ x.abs(), 3, "f32", "dw")
+    _close(db[1], c.sum(0), c.abs().sum(0), 3, "f32", "db")
+    _close(dx[-3:], c @ w[1].double(), c.abs() @ w[1].double().abs(), 64, "bf16", "dx")
+    assert not dw[0].any() and not dx[:-3].any()
+
+
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("counts", ["ragged", "edges"])
