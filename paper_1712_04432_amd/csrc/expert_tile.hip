@@ -7,8 +7,9 @@
 //   forward: m = o, n = s, k = i (both operands k-contiguous); Delta_X: m = i, n = s, k = o (W by k-rows);
 //   Delta_W: m = i, n = o, k = s (both by k-rows).
 //
-// A workgroup of four waves owns a 64 x 64 (or 64 x 32) tile of D and walks K in steps of 128 bytes a row, double-buffered
-// in LDS, with the loads of the next two steps (Delta_W: one) in flight over the products; rows of 144 bytes make every
+// A workgroup of four waves owns a 128 x 64, 64 x 64 or 64 x 32 tile of D and walks K in steps of 128 bytes a row, double-buffered
+// in LDS, with the loads of the next two steps (Delta_W, and the largest
+// tile: one) in flight over the products; rows of 144 bytes make every
 // fragment one conflict-free 16-byte read. Operands stored by k-rows are transposed in registers on their way.
 // Addresses are 64-bit and loads are 16 bytes at any element alignment, so no size or stride is special. Whole
 // steps load without conditions (rows that do not count from a row that exists); the last step of a K that is
@@ -22,31 +23,35 @@
 namespace imbd {
 namespace {
 
-constexpr int XT = 64;          // columns (m) of a tile
 constexpr int XT_PITCH = 144;   // bytes per LDS row
-constexpr int XT_OUT = XT + 4;  // staging row pitch in floats
 
-// 16 bytes from p; elements at index >= valid read as 0.
+// Elements pos .. pos + VEC - 1 of a run of `len` (those from len on are 0): the run's last VEC elements, moved down.
 template <typename T>
-__device__ __forceinline__ u32x4 chunk16(const T *p, int valid) {
-  constexpr int VEC = 16 / (int)sizeof(T);
-  if (valid >= VEC) return *reinterpret_cast<const u32x4_any *>(p);
-  T tmp[VEC];
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) tmp[e] = e < valid ? p[e] : T(0);
-  u32x4 r;
-  __builtin_memcpy(&r, tmp, 16);
-  return r;
+__device__ __forceinline__ u32x4 chunk16(const T *run, int pos, int len) {
+  constexpr int VEC = 16 / (int)sizeof(T), BITS = 8 * (int)sizeof(T);
+  unsigned __int128 v = 0;
+  if (len >= VEC) {
+    const int at = min(pos, len - VEC), by = pos - at;
+    v = __builtin_bit_cast(unsigned __int128, *reinterpret_cast<const u32x4_any *>(run + at));
+    v = by < VEC ? v >> (by * BITS) : 0;
+  } else {
+#pragma unroll 1
+    for (int e = len - 1; e >= pos; --e) {
+      if constexpr (sizeof(T) == 2) v = (v << BITS) | run[e];
+      else v = (v << BITS) | __builtin_bit_cast(uint32_t, run[e]);
+    }
+  }
+  return __builtin_bit_cast(u32x4, v);
 }
 
 // k-contiguous operand: R rows x 128 bytes, R/32 chunks a thread. row(r) gives row r's first element, or
 // null for a row of zeros; it does not change over k. `some`: any row that exists.
-template <typename T, int R>
+template <typename T, int R, int SETS>
 struct KcTile {
   static constexpr int VEC = 16 / (int)sizeof(T), PER = R / 32;
   const T *p[PER];
   bool ok[PER];
-  u32x4 v[2][PER];  // [register set][chunk]
+  u32x4 v[SETS][PER];  // [register set][chunk]
   template <typename F>
   __device__ __forceinline__ void init(F row, const T *some, int tid) {
 #pragma unroll
@@ -60,10 +65,13 @@ struct KcTile {
   template <bool G>
   __device__ __forceinline__ void load(int set, int k0, int K, int tid) {
     const int kk = k0 + (tid & 7) * VEC;
+    if constexpr (G) asm volatile("" : "+v"(K));  // (its addresses are not worth registers in the steps before)
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if constexpr (G) v[set][i] = ok[i] && kk < K ? chunk16<T>(p[i] + kk, K - kk) : u32x4{0u, 0u, 0u, 0u};
-      else v[set][i] = *reinterpret_cast<const u32x4_any *>(p[i] + kk);
+      if constexpr (G) {
+        v[set][i] = ok[i] && kk < K ? chunk16<T>(p[i], kk, K) : u32x4{0u, 0u, 0u, 0u};
+        __builtin_amdgcn_sched_barrier(0);  // (one after another: their shifts take registers)
+      } else v[set][i] = *reinterpret_cast<const u32x4_any *>(p[i] + kk);
     }
   }
   __device__ __forceinline__ void store(int set, char *lds, int tid) {
@@ -75,28 +83,51 @@ struct KcTile {
 };
 
 // Operand stored by k-rows: 128 bytes of k x R columns, in blocks of VEC x VEC transposed in registers, one a
-// thread of the first 8 R / VEC (`tid` is rotated so that two such operands use different waves). krow(j) gives
-// the first column of the tile in the thread's k-row j of the step, or null for zeros.
+// thread of the first 8 R / VEC (`tid` is rotated so that two such operands use different waves). A block that the
+// matrix's last column cuts is read `by` columns earlier, whole, and its first `by` columns, which are another
+// block's too, are not stored; what lies past the last column in LDS reaches only outputs that are not stored.
 template <typename T, int R, int SETS>
 struct TrTile {
   static constexpr int VEC = 16 / (int)sizeof(T);
   static constexpr int NB = 8 * R / VEC;
   u32x4 v[SETS][VEC];
+  int col, by;  // this thread's first column of the matrix
   __device__ __forceinline__ static int first_k(int tid) { return (tid & 7) * VEC; }
-  // G: with the columns' end looked at
-  template <bool G, typename F>
-  __device__ __forceinline__ void load(int set, F krow, const T *some, int cols, int tid) {
+  __device__ __forceinline__ void init(int col0, int width, int tid) {
+    const int c = col0 + (tid >> 3) * VEC;
+    col = width >= VEC ? min(c, width - VEC) : c;  // (narrower matrices: load_edge)
+    by = min(c - col, VEC);
+  }
+  // element by element. krow(j): the first element of the thread's k-row j, or null for zeros
+  template <typename F>
+  __device__ __forceinline__ void load_edge(int set, F krow, int width, int tid) {
     if (tid >= NB) return;
-    const int c = (tid >> 3) * VEC;
+    asm volatile("" : "+v"(width));
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
       const T *p = krow(j);
-      if constexpr (G) {
-        v[set][j] = p && c < cols ? chunk16<T>(p + c, cols - c) : u32x4{0u, 0u, 0u, 0u};
-      } else {
-        v[set][j] = *reinterpret_cast<const u32x4_any *>((p ? p : some) + c);
-        if (!p) v[set][j] = u32x4{0u, 0u, 0u, 0u};
-      }
+      v[set][j] = p && col < width ? chunk16<T>(p, col, width) : u32x4{0u, 0u, 0u, 0u};
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // rows ld apart from p on (which points at this thread's first column)
+  __device__ __forceinline__ void load_rows(int set, const T *p, int64_t ld, int tid) {
+    if (tid >= NB) return;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      v[set][j] = *reinterpret_cast<const u32x4_any *>(p);
+      p += ld;
+    }
+  }
+  // each row by its own pointer (null: zeros, read from `some`)
+  template <typename F>
+  __device__ __forceinline__ void load_each(int set, F krow, const T *some, int tid) {
+    if (tid >= NB) return;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const T *p = krow(j);
+      v[set][j] = *reinterpret_cast<const u32x4_any *>((p ? p : some) + col);
+      if (!p) v[set][j] = u32x4{0u, 0u, 0u, 0u};
     }
   }
   __device__ __forceinline__ void store(int set, char *lds, int tid) {
@@ -113,7 +144,8 @@ struct TrTile {
           o[q] = v[set][q][r];
         }
       }
-      *reinterpret_cast<u32x4 *>(lds + ((tid >> 3) * VEC + r) * XT_PITCH + (tid & 7) * 16) = o;
+      if (r >= by)
+        *reinterpret_cast<u32x4 *>(lds + ((tid >> 3) * VEC + r - by) * XT_PITCH + (tid & 7) * 16) = o;
     }
   }
 };
@@ -124,21 +156,21 @@ __device__ __forceinline__ bool positive(T v) {
   else return v > 0.f;
 }
 
-// TN: rows (n) of a tile, 64 or 32.
-template <typename T, int PASS, int TN>
+// TM, TN: columns (m) and rows (n) of a tile.
+template <typename T, int PASS, int TM, int TN>
 __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int tiles_m, int tiles_n) {
   constexpr int VEC = 16 / (int)sizeof(T);
   constexpr int BK = 8 * VEC;
-  constexpr int STAGE = (XT + TN) * XT_PITCH;
-  constexpr int FN = TN / 32;  // 16-row blocks of a wave (2 x 2 waves of 32 columns x TN/2 rows)
-  static_assert(TN * XT_OUT * 4 <= 2 * STAGE, "the staged tile reuses the operand buffers");
+  constexpr int STAGE = (TM + TN) * XT_PITCH;
+  constexpr int FM = TM / 32, FN = TN / 32;  // 16-wide blocks of a wave (2 x 2 waves)
+  constexpr int PT = TM + 4;                 // staging row pitch in floats
+  static_assert(TN * PT * 4 <= 2 * STAGE, "the staged tile reuses the operand buffers");
   __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
-  // each XCD takes a contiguous range of the launch order; column tiles run fastest, so that the tiles
-  // that share rows of x (or dy) follow each other
-  int bid = blockIdx.x;
-  if ((gridDim.x & 7) == 0) bid = (bid & 7) * (int)(gridDim.x >> 3) + (bid >> 3);
+  // the XCDs take 32 tiles of the launch order at a time by turns (experts of different length are spread over all);
+  // column tiles run fastest, so that the tiles that share rows of x (or dy) follow each other
+  const int turn = (int)(blockIdx.x >> 3), bid = ((turn >> 5) * 8 + (int)(blockIdx.x & 7)) * 32 + (turn & 31);
   const int tm = bid % tiles_m;
   int e, n0, n_end, r0 = 0, K;
   if constexpr (PASS == EXPERT_DW) {
@@ -152,7 +184,7 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
     if (!find_row_tile<TN>(a, bid / tiles_m, &e, &n0, &n_end)) return;
     K = PASS == EXPERT_FWD ? a.d_in : a.d_out;
   }
-  const int m0 = tm * XT, M = PASS == EXPERT_FWD ? a.d_out : a.d_in;
+  const int m0 = tm * TM, M = PASS == EXPERT_FWD ? a.d_out : a.d_in;
   const T *w = reinterpret_cast<const T *>(a.w) + (int64_t)e * a.sw;
   const T *x = reinterpret_cast<const T *>(a.x);
   const T *dy = reinterpret_cast<const T *>(a.dy);
@@ -161,23 +193,26 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
     return r >= 0 && r < a.n_x ? x + (int64_t)r * a.ldx : nullptr;
   };
 
-  constexpr int SETS = PASS == EXPERT_DW ? 1 : 2;  // register sets: steps whose loads are in flight
-  KcTile<T, XT> ka;
-  KcTile<T, TN> kb;
-  TrTile<T, XT, SETS> ta;
+  constexpr int SETS = PASS == EXPERT_DW || TM == 128 ? 1 : 2;  // register sets: steps whose loads are in flight
+  KcTile<T, TM, SETS> ka;
+  KcTile<T, TN, SETS> kb;
+  TrTile<T, TM, SETS> ta;
   TrTile<T, TN, SETS> tb;
   const int tid_b = tid ^ 128;  // (the k-row operand of n: the other half of the workgroup)
-  const int ka0 = TrTile<T, XT, SETS>::first_k(tid), kb0 = TrTile<T, TN, SETS>::first_k(tid_b);
-  // whether whole steps of k-rows may load without conditions: the tile's columns all exist
+  const int ka0 = TrTile<T, TM, SETS>::first_k(tid), kb0 = TrTile<T, TN, SETS>::first_k(tid_b);
+  // whether every block of the k-rows can be read whole
   bool inside = true;
   if constexpr (PASS == EXPERT_FWD) {
     ka.init([&](int r) { return m0 + r < M ? w + (int64_t)(m0 + r) * a.ldw : nullptr; }, w, tid);
     kb.init([&](int r) { return n0 + r < n_end ? x_row(n0 + r) : nullptr; }, a.n_x > 0 ? x : w, tid);
   } else if constexpr (PASS == EXPERT_DX) {
     kb.init([&](int r) { return n0 + r < n_end ? dy + (int64_t)(n0 + r) * a.lddy : nullptr; }, dy, tid);
-    inside = m0 + XT <= M;
+    ta.init(m0, M, tid);
+    inside = M >= VEC;
   } else {
-    inside = m0 + XT <= M && n0 + TN <= n_end && a.n_x > 0 && x != nullptr;
+    ta.init(m0, M, tid);
+    tb.init(n0, n_end, tid_b);
+    inside = M >= VEC && n_end >= VEC && a.n_x > 0 && x != nullptr;
   }
   // Delta_W: the rows of x of this thread's k-rows, read a step ahead of their use (read with it, every row's load
   // waited for its index and, loads coming back in order, for all loads before that)
@@ -191,38 +226,57 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
       }
     }
   };
+  // the k-rows of the next step, for whole steps (which come in order)
+  const T *wk = w + (int64_t)ka0 * a.ldw + ta.col, *yk = dy + (int64_t)(r0 + kb0) * a.lddy + tb.col;
+  const T *xk = x + (int64_t)(r0 + ka0) * a.ldx + ta.col;
+  // G: the step that holds the end of K
   auto load = [&](auto gtag, int set, int k0) {
     constexpr bool G = decltype(gtag)::value;
     if constexpr (PASS == EXPERT_FWD) ka.template load<G>(set, k0, K, tid);
     if constexpr (PASS != EXPERT_DW) kb.template load<G>(set, k0, K, tid);
-    if constexpr (PASS == EXPERT_DX)
-      ta.template load<G>(set, [&](int j) { return k0 + ka0 + j < K ? w + (int64_t)(k0 + ka0 + j) * a.ldw + m0 : nullptr; }, w,
-                          M - m0, tid);
+    int k_end = K;
+    if constexpr (G) asm volatile("" : "+s"(k_end), "+s"(k0));  // (as above)
+    if constexpr (PASS == EXPERT_DX) {
+      auto w_at = [&](int j) { return k0 + ka0 + j < k_end ? w + (int64_t)(k0 + ka0 + j) * a.ldw : nullptr; };
+      if (!G && inside) ta.load_rows(set, wk, a.ldw, tid);
+      else if (inside) ta.load_each(set, w_at, w, tid);
+      else ta.load_edge(set, w_at, M, tid);
+      wk += BK * a.ldw;
+    }
     if constexpr (PASS == EXPERT_DW) {
-      ta.template load<G>(set, [&](int j) { return xrow[j] >= 0 && xrow[j] < a.n_x ? x + (int64_t)xrow[j] * a.ldx + m0 : nullptr; },
-                          x + m0, M - m0, tid);
-      tb.template load<G>(set, [&](int j) { return k0 + kb0 + j < K ? dy + (int64_t)(r0 + k0 + kb0 + j) * a.lddy + n0 : nullptr; },
-                          dy, n_end - n0, tid_b);
+      auto x_at = [&](int j) { return xrow[j] >= 0 && xrow[j] < a.n_x ? x + (int64_t)xrow[j] * a.ldx : nullptr; };
+      auto y_at = [&](int j) { return k0 + kb0 + j < k_end ? dy + (int64_t)(r0 + k0 + kb0 + j) * a.lddy : nullptr; };
+      if (!inside) {
+        ta.load_edge(set, x_at, M, tid);
+        tb.load_edge(set, y_at, n_end, tid_b);
+      } else {
+        if (!G && !a.rows) ta.load_rows(set, xk, a.ldx, tid);
+        else ta.load_each(set, x_at, x, tid);
+        if (!G) tb.load_rows(set, yk, a.lddy, tid_b);
+        else tb.load_each(set, y_at, dy, tid_b);
+      }
+      xk += BK * a.ldx;
+      yk += BK * a.lddy;
       next_rows(k0 + BK);
     }
   };
   auto store = [&](int set, char *buf) {
     if constexpr (PASS == EXPERT_FWD) ka.store(set, buf, tid);
     else ta.store(set, buf, tid);
-    if constexpr (PASS != EXPERT_DW) kb.store(set, buf + XT * XT_PITCH, tid);
-    else tb.store(set, buf + XT * XT_PITCH, tid_b);
+    if constexpr (PASS != EXPERT_DW) kb.store(set, buf + TM * XT_PITCH, tid);
+    else tb.store(set, buf + TM * XT_PITCH, tid_b);
   };
 
-  const int wm = (wave & 1) * 32, wn = (wave >> 1) * (TN / 2), fr = lane & 15, fg = lane >> 4;
-  f32x4 acc[2][FN];
+  const int wm = (wave & 1) * (TM / 2), wn = (wave >> 1) * (TN / 2), fr = lane & 15, fg = lane >> 4;
+  f32x4 acc[FM][FN];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const bool do_db = PASS == EXPERT_DW && a.db && tm == 0;
   float dbsum = 0.f;
 
-  const int nk = (K + BK - 1) / BK, nw = inside ? K / BK : 0;  // steps; whole ones
+  const int nk = (K + BK - 1) / BK, nw = K / BK;  // steps; whole ones
   const std::integral_constant<bool, false> plain{};
   const std::integral_constant<bool, true> guarded{};
   auto fetch = [&](int set, int kt) {
@@ -231,19 +285,19 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
   };
   constexpr int DT = 256 / TN, DC = 8 / DT;  // db: threads a row, chunks a thread
   auto compute = [&](int kt) {
-    const char *sa = smem + (kt & 1) * STAGE, *sb = sa + XT * XT_PITCH;
+    const char *sa = smem + (kt & 1) * STAGE, *sb = sa + TM * XT_PITCH;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
-      u32x4 fa[2], fb[FN];
+      u32x4 fa[FM], fb[FN];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < FM; ++i)
         fa[i] = *reinterpret_cast<const u32x4 *>(sa + (wm + 16 * i + fr) * XT_PITCH + kk * 64 + fg * 16);
 #pragma unroll
       for (int j = 0; j < FN; ++j)
         fb[j] = *reinterpret_cast<const u32x4 *>(sb + (wn + 16 * j + fr) * XT_PITCH + kk * 64 + fg * 16);
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
           for (int j = 0; j < FN; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fa[i]),
@@ -252,7 +306,7 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
               const f32x4 af = __builtin_bit_cast(f32x4, fa[i]), bf = __builtin_bit_cast(f32x4, fb[j]);
@@ -304,12 +358,13 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
   // ---- the tile through LDS as [n][m], then rows of four outputs a thread
   float *stg = reinterpret_cast<float *>(smem);
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j)
-      *reinterpret_cast<f32x4 *>(stg + (wn + 16 * j + fr) * XT_OUT + wm + 16 * i + 4 * fg) = acc[i][j];
+      *reinterpret_cast<f32x4 *>(stg + (wn + 16 * j + fr) * PT + wm + 16 * i + 4 * fg) = acc[i][j];
   __syncthreads();
-  const int m = m0 + (tid & 15) * 4, cnt = min(4, M - m);
+  constexpr int TPR = TM / 4, RPP = 256 / TPR;  // threads a row, rows a pass
+  const int m = m0 + (tid % TPR) * 4, cnt = min(4, M - m);
   if (cnt <= 0) return;
   float bias[4] = {0.f, 0.f, 0.f, 0.f};
   if (PASS == EXPERT_FWD && a.bias) {
@@ -317,11 +372,11 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
     for (int q = 0; q < 4; ++q)
       if (q < cnt) bias[q] = a.bias[(int64_t)e * a.d_out + m + q];
   }
-#pragma unroll
-  for (int p = 0; p < TN / 16; ++p) {
-    const int nl = 16 * p + (tid >> 4), n = n0 + nl;
+#pragma unroll 2
+  for (int p = 0; p < TN / RPP; ++p) {
+    const int nl = RPP * p + tid / TPR, n = n0 + nl;
     if (n >= n_end) continue;
-    f32x4 v = *reinterpret_cast<const f32x4 *>(stg + nl * XT_OUT + (tid & 15) * 4);
+    f32x4 v = *reinterpret_cast<const f32x4 *>(stg + nl * PT + (tid % TPR) * 4);
     if constexpr (PASS == EXPERT_FWD) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -358,36 +413,46 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
 
 }  // namespace
 
-template <typename T, int TN>
+template <typename T, int TM, int TN>
 static int launch(int pass, const ExpertArgs &a, hipStream_t s) {
   const int M = pass == EXPERT_FWD ? a.d_out : a.d_in;
-  const int64_t tm = pass == EXPERT_DW && !a.out ? 1 : (M + XT - 1) / XT;  // (db alone: the first column of tiles)
+  const int64_t tm = pass == EXPERT_DW && !a.out ? 1 : (M + TM - 1) / TM;  // (db alone: the first column of tiles)
   const int64_t tn = (a.d_out + TN - 1) / TN;
   const int64_t blocks = (pass == EXPERT_DW ? a.E * tn : row_tiles_most(a.n_rows, a.E, TN)) * tm;
-  if (blocks >= ((int64_t)1 << 31) - 8) {
+  if (blocks >= ((int64_t)1 << 31) - 256) {
     set_error("expert product: %lld tiles are more than one launch takes", (long long)blocks);
     return IMBD_EUNSUPPORTED;
   }
   if (blocks == 0) return IMBD_OK;
-  const dim3 grid((unsigned)((blocks + 7) / 8 * 8)), wg(256);
+  const dim3 grid((unsigned)((blocks + 255) / 256 * 256)), wg(256);
   const int cm = (int)tm, cn = (int)tn;
   {
     LaunchTimer t(IMBD_K_EXPERT_FWD + pass, 0, s);
-    if (pass == EXPERT_FWD) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_FWD, TN>), grid, wg, 0, s, a, cm, cn);
-    else if (pass == EXPERT_DX) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DX, TN>), grid, wg, 0, s, a, cm, cn);
-    else hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DW, TN>), grid, wg, 0, s, a, cm, cn);
+    if (pass == EXPERT_FWD) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_FWD, TM, TN>), grid, wg, 0, s, a, cm, cn);
+    else if (pass == EXPERT_DX) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DX, TM, TN>), grid, wg, 0, s, a, cm, cn);
+    else hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DW, TM, TN>), grid, wg, 0, s, a, cm, cn);
   }
   return check_launch("expert_tile");
 }
 
-int run_expert_tile(int pass, int dtype, const ExpertArgs &a, hipStream_t s) {
-  // 32-row tiles where those of 64 do not give every CU four: whole workgroups come out more even, and more of them
-  // hide each other's waits. (The sums' order in K does not depend on the tile.)
+template <typename T>
+static int launch_sized(int pass, const ExpertArgs &a, hipStream_t s) {
+  // The largest tile that gives every CU two (128 x 64) or four (64 x 64) workgroups: a large one reads its operands
+  // less often, small ones come out more even and hide each other's waits. 16384 rows, 8 experts of 2047 x 2049, bf16:
+  // forward 341 us on 128 x 64 and 479 on 64 x 64, Delta_X 541 and 1436, Delta_W 678 and 1020 (fp32 Delta_W 1860 and
+  // 1586: it stays on the smaller); 3000 rows, 13 experts of 517 x 1023, fp32 forward 54 us on 64 x 32, 74 on 64 x 64.
   const int M = pass == EXPERT_FWD ? a.d_out : a.d_in;
-  const int64_t rows = pass == EXPERT_DW ? (int64_t)a.E * ((a.d_out + 63) / 64) : (int64_t)a.n_rows / 64 + a.E / 2;
-  const bool small = rows * ((M + XT - 1) / XT) < 1024;
-  if (dtype == IMBD_BF16) return small ? launch<uint16_t, 32>(pass, a, s) : launch<uint16_t, 64>(pass, a, s);
-  return small ? launch<float, 32>(pass, a, s) : launch<float, 64>(pass, a, s);
+  auto tiles = [&](int side) {
+    const int64_t rows = pass == EXPERT_DW ? (int64_t)a.E * ((a.d_out + side - 1) / side)
+                                           : (int64_t)a.n_rows / side + (a.n_rows < a.E ? a.n_rows : a.E) / 2;
+    return rows * ((M + side - 1) / side);
+  };
+  if ((sizeof(T) == 2 || pass != EXPERT_DW) && tiles(128) >= 256) return launch<T, 128, 64>(pass, a, s);
+  return tiles(64) >= 1024 ? launch<T, 64, 64>(pass, a, s) : launch<T, 64, 32>(pass, a, s);
+}
+
+int run_expert_tile(int pass, int dtype, const ExpertArgs &a, hipStream_t s) {
+  return dtype == IMBD_BF16 ? launch_sized<uint16_t>(pass, a, s) : launch_sized<float>(pass, a, s);
 }
 
 }  // namespace imbd
