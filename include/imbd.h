@@ -257,7 +257,8 @@ int conv3x3_tile_bwd(int N, int H, int W, int C_in, int C_out, const void *x_pad
  * index outside its array reads as zeros and writes nothing. One slot belongs to one expert
  * and to one (token, choice): where offsets overlap or slots name a slot twice, the outputs
  * there are undefined.
- * Sizes: 1 <= E <= 512 and 1 <= k <= 16; the number of slots and of tokens below 2^31.
+ * Sizes (IMBD_EUNSUPPORTED past them): 1 <= E <= 512 and 1 <= k <= 16; fewer than 2^31 - 1024
+ * slots, rows and tokens; widths up to 2^30. No output may overlap an input or another output.
  * ==================================================================================== */
 
 /* The router. logits [T][ldl] fp32, ldl >= E. Each token's k largest logits, in descending
@@ -352,8 +353,8 @@ typedef struct {
 
 /* The plan of a set of tensors: adamw_plan writes it to HOST memory (plan_bytes from
  * adamw_plan_bytes; 0 for a bad argument or a set without elements), the caller copies it to
- * device memory (16-byte aligned) once and keeps both it and the tensors where they are. No two
- * tensors of a set may share memory. */
+ * device memory (16-byte aligned) once and keeps both it and the tensors where they are. Tensors of
+ * a set that share memory are refused (gradients, which are only read, may share theirs). */
 size_t adamw_plan_bytes(const imbd_adamw_tensor *tensors, int n_tensors);
 int adamw_plan(const imbd_adamw_tensor *tensors, int n_tensors, void *plan, size_t plan_bytes);
 

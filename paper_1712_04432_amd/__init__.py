@@ -312,7 +312,8 @@ def expert_route(logits, gates, experts, offsets, rows, slots, ws=None, renorm: 
                            _sizes(experts, (T, k), i32, "experts", dev, True),
                            _sizes(offsets, (E + 1,), i32, "offsets", dev, True),
                            _sizes(rows, (T * k,), i32, "rows", dev, True),
-                           _sizes(slots, (T, k), i32, "slots", dev, True), None if ws is None else ws.data_ptr(),
+                           _sizes(slots, (T, k), i32, "slots", dev, True),
+                           None if ws is None else _sizes(ws, ws.shape, ws.dtype, "ws", dev, True),
                            0 if ws is None else ws.numel() * ws.element_size(), _on(stream, dev)), "expert_route")
 
 

@@ -50,7 +50,7 @@ __device__ __forceinline__ bool find_row_tile(const ExpertArgs &a, int t, int *e
     const int e = e0 + lane;
     int r0 = 0, cnt = 0;
     if (e < a.E) expert_range(a, e, &r0, &cnt);
-    const int tiles = (cnt + TR - 1) / TR;
+    const int tiles = cnt / TR + (cnt % TR != 0);
     int upto = tiles;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {

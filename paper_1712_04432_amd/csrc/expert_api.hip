@@ -1,6 +1,9 @@
 // C entry points of the expert layer and of AdamW (include/imbd.h): argument checks on the host, then one
 // call of the kernels' launch functions. No entry allocates, synchronises or throws.
 
+#include <stdlib.h>
+
+#include <algorithm>
 #include <cmath>
 
 #include "adamw.h"
@@ -14,6 +17,9 @@ namespace {
     set_error(__VA_ARGS__); \
     return (code);          \
   } while (0)
+
+// Row and column numbers plus a tile stay below 2^31.
+constexpr int ROWS_MOST = 0x7fffffff - 1024, WIDTH_MOST = 1 << 30;
 
 bool valid_dtype(int d) { return d == IMBD_F32 || d == IMBD_BF16; }
 
@@ -32,6 +38,8 @@ int check_layer(int dtype, int E, int d_out, int d_in, int n_rows, int n_x) {
     FAIL(IMBD_EINVAL, "bad expert sizes: E = %d, d_out = %d, d_in = %d, n_rows = %d, n_x = %d", E, d_out, d_in,
          n_rows, n_x);
   if (E > EXPERT_MAX) FAIL(IMBD_EUNSUPPORTED, "E = %d: at most %d experts", E, EXPERT_MAX);
+  if (n_rows > ROWS_MOST || n_x > ROWS_MOST || d_out > WIDTH_MOST || d_in > WIDTH_MOST)
+    FAIL(IMBD_EUNSUPPORTED, "n_rows = %d, n_x = %d, d_out = %d, d_in = %d", n_rows, n_x, d_out, d_in);
   return IMBD_OK;
 }
 
@@ -47,6 +55,49 @@ int check_combine(int dtype, int T, int k, int d, int n_rows) {
   if (T < 0 || k < 1 || d < 1 || n_rows < 0)
     FAIL(IMBD_EINVAL, "bad sizes: T = %d, k = %d, d = %d, n_rows = %d", T, k, d, n_rows);
   if (k > CHOICE_MAX) FAIL(IMBD_EUNSUPPORTED, "k = %d: at most %d", k, CHOICE_MAX);
+  if (T > ROWS_MOST || d > WIDTH_MOST) FAIL(IMBD_EUNSUPPORTED, "T = %d, d = %d", T, d);
+  return IMBD_OK;
+}
+
+struct Range {
+  uintptr_t from, to;
+  int tensor;
+  bool written;
+};
+
+// No tensor's memory in another's (or in its own twice): a step's workgroups run in any order.
+int check_apart(const imbd_adamw_tensor *t, int n) {
+  Range *r = static_cast<Range *>(malloc((size_t)n * 7 * sizeof(Range)));
+  if (!r) FAIL(IMBD_EINVAL, "no host memory to check %d tensors", n);
+  int count = 0;
+  for (int i = 0; i < n; ++i) {
+    const imbd_adamw_tensor &x = t[i];
+    if (x.n == 0) continue;
+    const size_t e = (size_t)x.n, s = x.state_bits == 8 ? 1 : 4, blocks = (e + 255) / 256;
+    auto add = [&](const void *p, size_t bytes, bool written) {
+      if (p) r[count++] = Range{(uintptr_t)p, (uintptr_t)p + bytes, i, written};
+    };
+    add(x.w, e * 4, true);
+    add(x.w_lp, e * 2, true);
+    add(x.grad, e * (x.grad_dtype == IMBD_BF16 ? 2 : 4), false);
+    add(x.m, e * s, true);
+    add(x.v, e * s, true);
+    if (x.state_bits == 8) {
+      add(x.m_scale, blocks * 4, true);
+      add(x.v_scale, blocks * 4, true);
+    }
+  }
+  std::sort(r, r + count, [](const Range &a, const Range &b) { return a.from < b.from; });
+  // against the furthest end so far, of all ranges and of the written ones
+  uintptr_t end = 0, end_written = 0;
+  int at = 0, bad = -1;
+  for (int i = 0; i < count && bad < 0; ++i) {
+    if (r[i].from < (r[i].written ? end : end_written)) bad = r[i].tensor;
+    if (r[i].to > end) end = r[i].to, at = r[i].tensor;
+    if (r[i].written && r[i].to > end_written) end_written = r[i].to;
+  }
+  free(r);
+  if (bad >= 0) FAIL(IMBD_EINVAL, "tensor %d shares memory with tensor %d", bad, at);
   return IMBD_OK;
 }
 
@@ -68,6 +119,10 @@ int check_tensors(const imbd_adamw_tensor *t, int n, size_t *bytes) {
     chunks += adamw_chunks(x.n);
   }
   if (chunks >= (int64_t)1 << 31) FAIL(IMBD_EUNSUPPORTED, "%lld chunks are more than one launch takes", (long long)chunks);
+  if (chunks > 0) {
+    const int rc = check_apart(t, n);
+    if (rc != IMBD_OK) return rc;
+  }
   if (chunks > 0) *bytes = (size_t)n * adamw_record_bytes() + (size_t)chunks * adamw_entry_bytes();
   return IMBD_OK;
 }

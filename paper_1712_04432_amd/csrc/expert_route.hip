@@ -218,8 +218,8 @@ __global__ void __launch_bounds__(RT_NT) choose_kernel(RouteArgs a) {
   if (SINGLE)
     for (int i = tid; i < a.E; i += RT_NT) sm[a.E + i] = 0;
   __syncthreads();
-  const int t0 = blockIdx.x * a.per_block, t1 = min(a.T, t0 + a.per_block);
-  for (int t = t0 + tid / G; t < t1; t += RT_NT / G) choose<G>(a, t, q, [&](int e) { atomicAdd(&sm[e], 1); });
+  const int t0 = blockIdx.x * a.per_block, t1 = (int)min((int64_t)a.T, (int64_t)t0 + a.per_block);
+  for (int64_t t = t0 + tid / G; t < t1; t += RT_NT / G) choose<G>(a, (int)t, q, [&](int e) { atomicAdd(&sm[e], 1); });
   __syncthreads();
   if constexpr (SINGLE) {
     __threadfence_block();
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(RT_NT) place_kernel(RouteArgs a) {
   }
   __syncthreads();
   starts(a, sm, sm + a.E, b == 0);
-  place(a, b * a.per_block, min(a.T, (b + 1) * a.per_block), sm + a.E, sm + 2 * a.E);
+  place(a, b * a.per_block, (int)min((int64_t)a.T, (int64_t)(b + 1) * a.per_block), sm + a.E, sm + 2 * a.E);
 }
 
 struct RouteBwdArgs {

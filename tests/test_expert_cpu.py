@@ -122,13 +122,33 @@ def test_adamw_plan_refuses(lib, bad):
     assert lib.adamw_plan(arr, 2, P, 1 << 20) == EINVAL
 
 
+@pytest.mark.parametrize("bad", [dict(w=4096), dict(w=4096 + 3996), dict(m=12288 + 4), dict(v=8192), dict(w_lp=16384 + 3998),
+                                 dict(w=20480, m=20480 + 100, v=24576), dict(grad=4096),
+                                 dict(state_bits=8, m=40000, v=41000, m_scale=42000, v_scale=42008)])
+def test_adamw_plan_refuses_shared_memory(lib, bad):
+    """Against a tensor of 1000 elements at 4096 (w), 8192 (gradient), 12288 and 16384 (states)."""
+    apart = dict(w=1 << 20, grad=1 << 21, m=1 << 22, v=1 << 23)
+    arr = _array(_tensor(**{**apart, **bad}), _tensor())
+    assert lib.adamw_plan_bytes(arr, 2) == 0
+    assert lib.adamw_plan(arr, 2, P, 1 << 20) == EINVAL and b"shares memory" in lib.imbd_last_error()
+    for ok in (apart, {**apart, "grad": 8192}):  # (a gradient that two tensors read)
+        assert lib.adamw_plan_bytes(_array(_tensor(**ok), _tensor()), 2) > 0
+
+
+@pytest.mark.parametrize("bad", [dict(n_rows=2 ** 31 - 1, n_x=2 ** 31 - 1), dict(n_x=2 ** 31 - 1),
+                                 dict(d_out=2 ** 30 + 8, ldy=2 ** 31, sw=2 ** 40), dict(d_in=2 ** 30 + 8, ldw=2 ** 31, ldx=2 ** 31, sw=2 ** 40)])
+def test_fwd_refuses_sizes_past_32_bits(lib, bad):
+    assert lib.expert_fwd(*{**FWD, **bad}.values(), None) == EUNSUPPORTED
+
+
 def test_adamw_plan(lib):
     """The plan covers every tensor once, whatever their sizes, and tensors of no elements cost nothing."""
     assert lib.adamw_plan_bytes(None, 0) == 0 and lib.adamw_plan(None, 0, None, 0) == OK
     assert lib.adamw_plan_bytes(None, 1) == 0 and lib.adamw_plan_bytes(_array(_tensor()), -1) == 0
     assert lib.adamw_plan_bytes(_array(_tensor(n=0, w=None)), 1) == 0
     one = lib.adamw_plan_bytes(_array(_tensor(n=1)), 1)
-    arr = _array(_tensor(n=0), _tensor(n=100000), _tensor(n=1))
+    big = dict(w=1 << 30, grad=1 << 31, m=1 << 32, v=1 << 33)
+    arr = _array(_tensor(n=0), _tensor(n=100000, **big), _tensor(n=1))
     need = lib.adamw_plan_bytes(arr, 3)
     assert need > one > 0
     buf = np.zeros(need + 8, np.uint8)

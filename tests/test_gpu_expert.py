@@ -750,3 +750,59 @@ def test_on_another_stream(imbd, dev):
     imbd.expert_fwd(L.w, L.x, L.offsets, y2, stream=s)
     s.synchronize()
     assert torch.equal(y, y2)
+
+
+def test_refusals(imbd, dev):
+    """What does not fit together is refused before anything is launched."""
+    import torch
+    L = Layer(dev, [3, 5], 64, 32, "bf16", gather=True, seed=1)
+    y = torch.full((8, 64), 7.0, dtype=torch.bfloat16, device=dev)
+    for bad in (dict(w=L.w[:, :, :-1]), dict(w=L.w[:1]), dict(x=L.x.float()), dict(x=L.x.cpu()), dict(offsets=L.offsets.long()),
+                dict(offsets=L.offsets[:-1]), dict(rows=L.rows[:-1]), dict(rows=L.rows.long()), dict(bias=L.bias.half()),
+                dict(bias=L.bias[:, :-1]), dict(y=y[:, ::2]), dict(y=y.half()), dict(w=L.w.transpose(1, 2)), dict(w=L.w.cpu()),
+                dict(x=L.x[:1].expand(L.n_x, 32)), dict(w=L.w[:1].expand(2, 64, 32)), dict(rows=None)):
+        a = {**dict(w=L.w, x=L.x, offsets=L.offsets, y=y, bias=L.bias, rows=L.rows), **bad}
+        with pytest.raises((ValueError, TypeError, imbd.ImbdError)):
+            imbd.expert_fwd(**a)
+    dw, db = torch.full((2, 64, 32), 7.0, device=dev), torch.full((2, 64), 7.0, device=dev)
+    for bad in (dict(dw=dw[:1]), dict(dw=dw.bfloat16()), dict(db=db[:, 1:]), dict(dy=L.dy[:, :-1]), dict(x=None),
+                dict(dw=None, db=None), dict(dx=torch.empty(8, 31, device=dev)), dict(dx=torch.empty(8, 32, device=dev).double())):
+        a = {**dict(w=L.w, dy=L.dy, x=L.x, offsets=L.offsets, dw=dw, db=db, rows=L.rows), **bad}
+        with pytest.raises((ValueError, TypeError, imbd.ImbdError)):
+            imbd.expert_bwd(**a)
+    z = torch.zeros(1000, 8, device=dev)
+    f, i = lambda *s: torch.zeros(*s, device=dev), lambda *s: torch.zeros(*s, dtype=torch.int32, device=dev)  # noqa: E731
+    ok = dict(logits=z, gates=f(1000, 2), experts=i(1000, 2), offsets=i(9), rows=i(2000), slots=i(1000, 2),
+              ws=torch.zeros(imbd.expert_route_workspace_bytes(1000, 8, 2), dtype=torch.uint8, device=dev))
+    imbd.expert_route(**ok)
+    for bad in (dict(ws=None), dict(ws=ok["ws"][:-1]), dict(ws=ok["ws"].cpu()), dict(logits=z.double()), dict(gates=f(1000, 9)),
+                dict(experts=ok["experts"].long()), dict(offsets=i(8)), dict(rows=i(1999)), dict(slots=i(2, 1000).t())):
+        with pytest.raises((ValueError, TypeError, imbd.ImbdError)):
+            imbd.expert_route(**{**ok, **bad})
+    with pytest.raises(ValueError):
+        imbd.expert_combine(y, i(4, 2), torch.empty(3, 64, device=dev))
+    with pytest.raises(ValueError):
+        imbd.expert_combine_bwd(y[:4], y, i(4, 2), f(4, 2), y[:, :-1])
+    torch.cuda.synchronize()
+    assert (y == 7.0).all() and (dw == 7.0).all() and (db == 7.0).all()
+
+
+def test_two_streams_at_once(imbd, dev):
+    """Calls on two streams share nothing: both give the bits that they give alone."""
+    import torch
+    Ls = [Layer(dev, [700, 0, 900], 512, 256, "bf16", gather=True, seed=s) for s in (1, 2)]
+    alone = []
+    for L in Ls:
+        y = torch.zeros(L.n, 512, dtype=torch.bfloat16, device=dev)
+        imbd.expert_fwd(L.w, L.x, L.offsets, y, bias=L.bias, rows=L.rows)
+        alone.append(y)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in Ls]
+    outs = [torch.zeros_like(y) for y in alone]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for L, s, y in zip(Ls, streams, outs):
+            with torch.cuda.stream(s):
+                imbd.expert_fwd(L.w, L.x, L.offsets, y, bias=L.bias, rows=L.rows)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(alone, outs))
