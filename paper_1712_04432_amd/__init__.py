@@ -38,9 +38,15 @@ __all__ = [
 ]
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def dtype_code(t_or_dtype) -> int:
@@ -254,30 +260,31 @@ def conv3x3_tile_bwd(x_pad, w, dy_pad, dw, dx=None, ws=None, stream=None):
 # tensors are checked against each other here (ValueError, TypeError); everything else is
 # checked by the library (ImbdError).
 def _sizes(t, shape, dtype, name, device, whole=False):
-    """Shape, type, device and layout of one tensor: rows without gaps between elements, or
-    (whole) contiguous. Returns its address."""
+    """Shape, type, device (its index) and layout of one tensor: rows without gaps between elements,
+    or (whole) contiguous. Returns its address."""
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple(shape)}")
     if t.dtype is not dtype:
         raise TypeError(f"{name}: {t.dtype}, need {dtype}")
-    if t.device != device:
-        raise ValueError(f"{name}: on {t.device}, need {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, need cuda:{device}")
     if not t.is_contiguous() and (whole or (t.shape[-1] > 1 and t.stride(-1) != 1)):
         raise ValueError(f"{name}: strides {t.stride()}")
     return t.data_ptr()
 
 
 def _here(t, name):
-    """The tensor's device, which has to be the current one (the stream is taken from it)."""
-    dev = t.device
-    if dev.type != "cuda" or dev.index != _torch().cuda.current_device():
-        raise ValueError(f"{name}: on {dev}, which is not the current device")
+    """The index of the tensor's device, which has to be the current one (the stream is taken from
+    it)."""
+    dev = t.get_device()
+    if dev < 0 or dev != _torch()._C._cuda_getDevice():
+        raise ValueError(f"{name}: on {t.device}, which is not the current device")
     return dev
 
 
 def _on(stream, device):
     """The address of a stream, or of the device's current one."""
-    return _torch()._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+    return _torch()._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def _rows_ld(t):
@@ -418,7 +425,7 @@ class AdamW:
         tensors = [dict(t) for t in tensors]
         self.tensors = tensors
         arr = (AdamWTensor * max(len(tensors), 1))()
-        dev = _here(tensors[0]["w"], "w") if tensors else torch.device("cuda", torch.cuda.current_device())
+        dev = _here(tensors[0]["w"], "w") if tensors else torch.cuda.current_device()
         f32 = torch.float32
         for a, t in zip(arr, tensors):
             w, n = t["w"], t["w"].numel()
@@ -444,7 +451,7 @@ class AdamW:
         host = torch.empty(max(self.bytes, 8), dtype=torch.uint8)
         # (a plan of no bytes: nothing to update, or a bad argument, which this call reports)
         check(lib.adamw_plan(arr, len(tensors), _ptr(host), self.bytes), "adamw_plan")
-        self.plan = host.to(dev)
+        self.plan = host.to(torch.device("cuda", dev))
         self.address = self.plan.data_ptr()
 
 
@@ -454,8 +461,8 @@ def adamw_step(plan: AdamW, lr: float, beta1: float = 0.9, beta2: float = 0.999,
     tensor that holds it (read by the kernel, so a captured launch follows it)."""
     lib, torch = load(), _torch()
     dev = plan.device
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"plan: on {dev}, which is not the current device")
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError(f"plan: on cuda:{dev}, which is not the current device")
     dev_step = None
     if not isinstance(step, int):
         dev_step = _sizes(step, step.shape, torch.int32, "step", dev, True)
