@@ -139,6 +139,10 @@ struct Shape {
   static constexpr int loads(int h) { return la(h) + lb(h); }
 };
 
+// Delta_X on 128-row tiles has room for the tile's mask beside its slots: it is loaded first of all and waits there (64
+// experts of 2048 x 1024: its loads in the epilogue took 23 of 132 us).
+constexpr bool xw_mask_in_lds(int PASS, int BN) { return PASS == EXPERT_DX && BN == 128; }
+
 // A wave's part of LDS in the epilogue: its outputs as bf16, half of them as fp32.
 constexpr int xw_stage_bytes(int BM, int BN) { return BM / 2 * (BN / 2) * 2; }
 
@@ -147,7 +151,7 @@ constexpr int xw_lds_bytes() {
   // the slots; Delta_W with gathered x: the row indices of eight half slabs, 256 bytes a wave each
   constexpr int ring = Shape<PASS, BM, BN>::RING + (PASS == EXPERT_DW && GATHER ? 8 * 1024 : 0);
   constexpr int stage = 4 * xw_stage_bytes(BM, BN);
-  return ring > stage ? ring : stage;
+  return (ring > stage ? ring : stage) + (xw_mask_in_lds(PASS, BN) ? BM * BN * 2 : 0);
 }
 
 // ES: bytes of an output (a kernel for each: with both in one, the sums were copied ahead of the branch, and spilled)
@@ -384,6 +388,21 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
     for (int j = 0; j < FN; ++j) accd[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
 
+  // ---- a wave's part of the mask: four rows a load, each lane what it will store with (rows in expert order; of
+  // gathered ones it is loaded in the epilogue)
+  constexpr bool MASK_LDS = xw_mask_in_lds(PASS, BN);
+  const uint32_t mask0 = lds0 + (uint32_t)(xw_lds_bytes<PASS, BM, BN, GATHER>() - BM * BN * 2 + wave * (BM * BN / 2));
+  if constexpr (MASK_LDS) {
+    const int mw = m0 + wm * (BM / 2), nw = n0 + wn * (BN / 2), left = min(BN / 2, n_end - nw);
+    if (a.mask && !a.rows && left > 0 && mw < M) {
+      const i32x4 rm = buf_rsrc(x + (int64_t)nw * a.ldx + mw, (uint32_t)(((int64_t)(left - 1) * a.ldx + min(BM / 2, M - mw)) * 2));
+      const uint32_t c = mw + 8 * fi < M ? (uint32_t)(16 * fi) : XW_OOB;
+#pragma unroll
+      for (int q = 0; q < BN / 8; ++q)
+        dma16(rm, c == XW_OOB ? XW_OOB : (uint32_t)(4 * q + kg) * (uint32_t)(a.ldx * 2) + c, mask0 + (uint32_t)(q * 1024));
+    }
+  }
+
   // ---- the first two slabs (and the indices of eight half slabs)
   const std::integral_constant<int, 0> c0{};
   const std::integral_constant<int, 1> c1{};
@@ -542,6 +561,13 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
 #pragma unroll
           for (int q = 0; q < BATCH; ++q) {
             const int r = (g * BATCH + q) * RPI + row0;
+            if constexpr (MASK_LDS) {
+              if (!a.rows) {
+                mk[g & 1][q] = *(const __attribute__((address_space(3))) MaskVec *)(uintptr_t)(
+                    mask0 + (uint32_t)((r >> 2) * 1024 + (r & 3) * 256 + ch * (32 / ES)));
+                continue;
+              }
+            }
             int row = -1;
             if (r < rows_left && col != XW_OOB) row = a.rows ? a.rows[nw + r] : nw + r;
             mk[g & 1][q] = MaskVec{};
