@@ -7,14 +7,18 @@
 //   forward: m = o, n = s, k = i (both operands k-contiguous); Delta_X: m = i, n = s, k = o (W by k-rows);
 //   Delta_W: m = i, n = o, k = s (both by k-rows).
 //
-// A workgroup of four waves owns a 128 x 64, 64 x 64 or 64 x 32 tile of D and walks K in steps of 128 bytes a row, double-buffered
-// in LDS, with the loads of the next two steps (Delta_W, and the largest
-// tile: one) in flight over the products; rows of 144 bytes make every
-// fragment one conflict-free 16-byte read. Operands stored by k-rows are transposed in registers on their way.
+// A workgroup of four waves owns a 128 x 64, 64 x 64 or 64 x 32 tile of D and walks K in steps of 128 bytes a row,
+// double-buffered in LDS, with the loads of the next two steps (Delta_W, and the largest tile: one) in flight over the
+// products; rows of 144 bytes make every fragment one conflict-free 16-byte read. Operands stored by k-rows are transposed in registers on their way.
 // Addresses are 64-bit and loads are 16 bytes at any element alignment, so no size or stride is special. Whole
 // steps load without conditions (rows that do not count from a row that exists); the last step of a K that is
 // no whole number of them, and k-rows at the edge of their matrix, chunk by chunk and element by element.
 // fp32 operands run on the fp32 matrix instruction: products and sums are fp32 for both types.
+//
+// Measured, 16384 rows, 8 experts of 2047 x 2049: bf16 forward 403 TFLOP/s, Delta_X 254, Delta_W 203 (111 with gathered
+// rows), fp32 98, 88 and 87; bound by the latency of the steps with two workgroups a CU. bf16 Delta_W needs 230 to 250
+// registers for its two transposes and both ways of reading a row; a form with 120, which read blocks cut by the last
+// column element by element, ran at 237 (160 gathered).
 
 #include <type_traits>
 

@@ -14,8 +14,11 @@
 //    weight gradient took 13% longer);
 //  * the fragments of a k-step are read between the products of the one before, into a second register set;
 //  * one barrier a k-step (a slab, where both operands have k contiguous: one of them then has three slots, so that
-//    their loads take turns; all in one k-step, the loads themselves waited for their place), at which the wave's next products
-//    already have their operands in registers.
+//    their loads take turns; all in one k-step, the loads themselves waited for their place), at which the wave's next
+//    products already have their operands in registers.
+// Measured, 16384 tokens, k = 2, 8 experts of 4096 x 4096: forward 786 to 821 us, Delta_X and Delta_W together 1635 to
+// 1710 (1.3 to 1.4 PFLOP/s; a library product of 8192 x 4096 x 4096 reaches 1.56). The matrix cores are busy 68 to 72%
+// of the cycles; the rest is the last, partial round of tiles and the start and end of each.
 //
 // Slabs in LDS. An operand with k contiguous: rows of 128 bytes, the 16-byte chunks XORed with row%8. By k-rows:
 // quarters of 64 columns, 64 k-rows of 128 bytes, read with the LDS transpose read; its swizzle is that of the
@@ -534,7 +537,8 @@ __global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int
   }
 
   // ---- epilogue: each wave puts its outputs through its own part of LDS ([n][m], 16-byte chunks XORed with the row)
-  // and stores whole rows, 16 bytes a lane, past the caches (537 MB of gradients of few rows: 131 -> 109 us); what lies outside the tile's rows or columns is past the descriptor.
+  // and stores whole rows, 16 bytes a lane, past the caches (537 MB of gradients of few rows: 131 -> 109 us); what lies
+  // outside the tile's rows or columns is past the descriptor.
   constexpr int WM = BM / 2, WN = BN / 2;  // columns, rows of a wave
   const int mw = m0 + wm * WM, nw = n0 + wn * WN;
   const uint32_t stg = lds0 + (uint32_t)(wave * xw_stage_bytes(BM, BN));
