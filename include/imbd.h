@@ -367,7 +367,7 @@ int adamw_plan(const imbd_adamw_tensor *tensors, int n_tensors, void *plan, size
  * with step_dev != NULL the device int32 that it points to: a captured launch then follows the
  * caller's counter.
  * State of 8 bits, in blocks of 256 elements: m is held as float8 e4m3 times m_scale =
- * max|m| * (1/448) of the block, rounded to nearest; v as float8 e5m2 times v_scale =
+ * max|m| * (1/448) of the block, rounded to nearest, 448 at most; v as float8 e5m2 times v_scale =
  * max v * (1/57344), rounded up or down by a dither of the element's index and t (a second moment
  * that moves by 1 - beta2 a step would stay where it is if rounded to nearest), and never to zero:
  * what is positive and under the smallest normal number is held as that number (2^-14). The update

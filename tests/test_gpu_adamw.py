@@ -217,6 +217,30 @@ def test_non_finite_gradients(imbd, dev):
             assert not torch.isfinite(a[300]) and not torch.isfinite(a[700])
 
 
+def test_a_first_moment_that_decays_to_nothing(imbd, dev):
+    """Without gradients m shrinks by beta1 a step until its scale is a few of the smallest fp32 numbers (u = 2^-149),
+    where the scale is rounded by up to a third. Against the exact m: half a code's step (16 scales), what lies past
+    448 scales, and the fp32 roundings of the code times its scale and of the product with beta1 (u / 2 each)."""
+    import torch
+    nb, u = 64, 2.0 ** -149
+    t = dict(w=torch.randn(256 * nb, device=dev), grad=torch.zeros(256 * nb, device=dev),
+             m=torch.full((256 * nb,), 0x7E, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn),
+             v=torch.full((256 * nb,), 0x7B, dtype=torch.uint8, device=dev).view(torch.float8_e5m2),
+             m_scale=(torch.arange(1, nb + 1, device=dev).double() * u).float(),
+             v_scale=torch.full((nb,), 1e-6, device=dev), decay=0.0)
+    t["m"].view(torch.uint8)[1::2] |= 0x80
+    plan, w = imbd.AdamW([t]), t["w"].clone()
+    for step in range(900, 960):
+        exact = _values(t, "m") * HYPER["beta1"]
+        imbd.adamw_step(plan, step=step, **HYPER)
+        got, s = _values(t, "m"), t["m_scale"].double().repeat_interleave(256)
+        assert torch.isfinite(got).all()
+        bound = 16 * s + (exact.abs() - 448 * s).clamp(min=0) + u
+        bound = torch.where(s == 0, exact.abs() + u, bound)
+        assert ((got - exact).abs() <= bound).all(), step
+    assert torch.equal(t["w"], w)  # (steps of 1e-40)
+
+
 def test_step_from_device_and_graph(imbd, dev):
     """The step's number in device memory: the bits of the same number as an argument, and a replayed graph follows
     the counter."""
