@@ -258,7 +258,8 @@ int conv3x3_tile_bwd(int N, int H, int W, int C_in, int C_out, const void *x_pad
  * and to one (token, choice): where offsets overlap or slots name a slot twice, the outputs
  * there are undefined.
  * Sizes (IMBD_EUNSUPPORTED past them): 1 <= E <= 512 and 1 <= k <= 16; fewer than 2^31 - 1024
- * slots, rows and tokens; widths up to 2^30. No output may overlap an input or another output.
+ * slots, rows and tokens; widths up to 2^30; and no launch of 2^24 workgroups or more: a tile of
+ * rows, 4 tokens (expert_combine_bwd), 4 to 32 tokens (expert_route_bwd). No output may overlap an input or another output.
  * ==================================================================================== */
 
 /* The router. logits [T][ldl] fp32, ldl >= E. Each token's k largest logits, in descending

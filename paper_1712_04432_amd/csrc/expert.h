@@ -7,6 +7,8 @@ namespace imbd {
 
 constexpr int EXPERT_MAX = 512;  // experts
 constexpr int CHOICE_MAX = 16;   // experts per token
+// Workgroups of 256 threads a launch may have: its work-items are a 32-bit number.
+constexpr int64_t WORKGROUPS_MOST = ((int64_t)1 << 24) - 1;
 
 // One grouped product. fwd: out = W x (rows n x d_out); dx: out = W^T dy (rows n x d_in); dw: out_e =
 // dy^T x per expert. Pointers and strides as in include/imbd.h.

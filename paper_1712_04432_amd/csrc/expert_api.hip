@@ -28,6 +28,7 @@ int check_route(int T, int E, int k) {
   if (k > E) FAIL(IMBD_EINVAL, "k = %d experts of E = %d", k, E);
   if (E > EXPERT_MAX || k > CHOICE_MAX)
     FAIL(IMBD_EUNSUPPORTED, "E = %d, k = %d: at most %d experts and %d a token", E, k, EXPERT_MAX, CHOICE_MAX);
+  if (T > ROWS_MOST) FAIL(IMBD_EUNSUPPORTED, "T = %d", T);
   if ((int64_t)T * k >= (int64_t)1 << 31) FAIL(IMBD_EUNSUPPORTED, "T * k = %lld pairs", (long long)T * k);
   return IMBD_OK;
 }
@@ -118,7 +119,7 @@ int check_tensors(const imbd_adamw_tensor *t, int n, size_t *bytes) {
     if (adamw_chunks(x.n) > 0xffffffffll) FAIL(IMBD_EUNSUPPORTED, "tensor %d: n = %lld", i, (long long)x.n);
     chunks += adamw_chunks(x.n);
   }
-  if (chunks >= (int64_t)1 << 31) FAIL(IMBD_EUNSUPPORTED, "%lld chunks are more than one launch takes", (long long)chunks);
+  if (chunks > WORKGROUPS_MOST) FAIL(IMBD_EUNSUPPORTED, "%lld chunks are more than one launch takes", (long long)chunks);
   if (chunks > 0) {
     const int rc = check_apart(t, n);
     if (rc != IMBD_OK) return rc;
@@ -288,7 +289,7 @@ int adamw_step(const void *plan, size_t plan_bytes, int n_tensors, double lr, do
   if (plan_bytes <= head || (plan_bytes - head) % adamw_entry_bytes())
     FAIL(IMBD_EINVAL, "plan_bytes = %zu is no plan of %d tensors", plan_bytes, n_tensors);
   const size_t chunks = (plan_bytes - head) / adamw_entry_bytes();
-  if (n_tensors == 0 || chunks >= (size_t)1 << 31) FAIL(IMBD_EINVAL, "plan_bytes = %zu is no plan", plan_bytes);
+  if (n_tensors == 0 || chunks > (size_t)WORKGROUPS_MOST) FAIL(IMBD_EINVAL, "plan_bytes = %zu is no plan", plan_bytes);
   return run_adamw(plan, n_tensors, (int64_t)chunks, lr, beta1, beta2, eps, grad_scale, step, step_dev,
                    stream_of(stream));
 }

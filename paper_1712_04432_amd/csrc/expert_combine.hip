@@ -155,7 +155,12 @@ int run_combine_bwd(int dtype, int T, int k, int d, int n_rows, const void *dy, 
   a.dy = dy; a.lddy = lddy; a.dys = dys; a.lddys = lddys; a.dgates = dgates;
   const size_t es = dtype == IMBD_BF16 ? 2 : 4;
   const bool vec = d % 8 == 0 && al16(dy, lddy, es) && al16(dys, lddys, es) && (!dgates || al16(ys, ldys, es));
-  const dim3 grid((unsigned)(((int64_t)T + 3) / 4)), wg(256);
+  const int64_t blocks = ((int64_t)T + 3) / 4;
+  if (blocks > WORKGROUPS_MOST) {
+    set_error("expert_combine_bwd: T = %d tokens are more than one launch takes", T);
+    return IMBD_EUNSUPPORTED;
+  }
+  const dim3 grid((unsigned)blocks), wg(256);
   {
     LaunchTimer t(IMBD_K_COMBINE, 1, s);
     if (dtype == IMBD_BF16) {

@@ -103,7 +103,7 @@ int run_expert_few(const ExpertArgs &a, hipStream_t s) {
   const int64_t t32 = (a.d_out + 31) / 32, t16 = (a.d_out + 15) / 16;
   const bool wide = rows * t32 >= 512;
   const int64_t blocks = rows * (wide ? t32 : t16);
-  if (blocks >= (int64_t)1 << 31) {
+  if (blocks > WORKGROUPS_MOST) {
     set_error("expert product: %lld tiles are more than one launch takes", (long long)blocks);
     return IMBD_EUNSUPPORTED;
   }

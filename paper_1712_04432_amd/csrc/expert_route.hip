@@ -8,11 +8,11 @@
 // ties go to the lowest expert whatever the lanes do. Selection compares the logits themselves, never
 // rounded probabilities.
 //
-// Ordering. A stable counting sort without atomics on the result: workgroup b (RT_TOKENS tokens) counts
+// Ordering. A stable counting sort without atomics on the result: workgroup b (128 tokens, or more so that there are at most 256) counts
 // its pairs per expert into row b of a table in ws; the second launch adds up the rows before its own for
 // the start of its pairs of each expert, and numbers its pairs in order, 64 at a time in a wave (a pair's
 // rank among the lanes of its expert comes from one ballot for each bit of the expert's index). Up to
-// RT_TOKENS tokens one workgroup does both in one launch.
+// 128 tokens one workgroup does both in one launch.
 //
 // Bound by latency: 16384 tokens, 64 experts, k = 8 move 11 MB (2.3 us) and take 7.6 us for the choice, 4.8 for the
 // order and 4.4 for the logits' gradient; 16 tokens, k = 4, 4.8 us in one launch.
@@ -388,7 +388,12 @@ int run_route_bwd(int T, int E, int k, int renorm, const float *logits, int64_t 
   if (T == 0) return IMBD_OK;
   RouteBwdArgs a{T, E, k, renorm, logits, ldl, gates, dgates, experts, dlogits, lddl};
   const int G = E <= 64 ? 8 : E <= 128 ? 16 : E <= 256 ? 32 : 64, per = 256 / G;
-  const dim3 grid((unsigned)(((int64_t)T + per - 1) / per)), wg(256);
+  const int64_t blocks = ((int64_t)T + per - 1) / per;
+  if (blocks > WORKGROUPS_MOST) {
+    set_error("expert_route_bwd: T = %d tokens are more than one launch takes", T);
+    return IMBD_EUNSUPPORTED;
+  }
+  const dim3 grid((unsigned)blocks), wg(256);
   {
     LaunchTimer t(IMBD_K_ROUTE, 2, s);
 #define GO(G_)                                                                           \

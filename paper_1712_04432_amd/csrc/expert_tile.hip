@@ -423,7 +423,7 @@ static int launch(int pass, const ExpertArgs &a, hipStream_t s) {
   const int64_t tm = pass == EXPERT_DW && !a.out ? 1 : (M + TM - 1) / TM;  // (db alone: the first column of tiles)
   const int64_t tn = (a.d_out + TN - 1) / TN;
   const int64_t blocks = (pass == EXPERT_DW ? a.E * tn : row_tiles_most(a.n_rows, a.E, TN)) * tm;
-  if (blocks >= ((int64_t)1 << 31) - 256) {
+  if (blocks > WORKGROUPS_MOST - 255) {
     set_error("expert product: %lld tiles are more than one launch takes", (long long)blocks);
     return IMBD_EUNSUPPORTED;
   }

@@ -660,7 +660,7 @@ static int launch(const ExpertArgs &a, hipStream_t s) {
   const int64_t tm = PASS == EXPERT_DW && !a.out ? 1 : (M + BM - 1) / BM;
   const int64_t tn = (a.d_out + BN - 1) / BN;
   const int64_t rows = row_tiles_most(a.n_rows, a.E, BN), blocks = (PASS == EXPERT_DW ? a.E * tn : rows) * tm;
-  if (blocks >= ((int64_t)1 << 31) - 256) {
+  if (blocks > WORKGROUPS_MOST - 255) {
     set_error("expert product: %lld tiles are more than one launch takes", (long long)blocks);
     return IMBD_EUNSUPPORTED;
   }

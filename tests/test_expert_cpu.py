@@ -141,6 +141,18 @@ def test_fwd_refuses_sizes_past_32_bits(lib, bad):
     assert lib.expert_fwd(*{**FWD, **bad}.values(), None) == EUNSUPPORTED
 
 
+def test_refuses_more_than_a_launch_takes(lib):
+    """2^24 workgroups of 256 threads are 2^32 work-items."""
+    tiles = dict(E=1, d_out=1, d_in=1, n_rows=2 ** 30, n_x=2 ** 30, rows=None, dtype=0, y_dtype=0, ldy=1, ldw=1, ldx=1)
+    assert lib.expert_fwd(*{**FWD, **tiles}.values(), None) == EUNSUPPORTED
+    T = 2 ** 29
+    assert lib.expert_route_bwd(T, 8, 2, 1, None, 8, P, P, P, P, 8, None) == EUNSUPPORTED
+    assert lib.expert_combine_bwd(0, T, 2, 8, 100, P, 8, P, 8, P, P, P, 8, P, None) == EUNSUPPORTED
+    assert _route(lib, T=2 ** 31 - 1, k=1) == EUNSUPPORTED
+    big = _array(_tensor(n=2 ** 37, w=1 << 42, grad=1 << 43, m=1 << 44, v=1 << 45))
+    assert lib.adamw_plan_bytes(big, 1) == 0 and lib.adamw_plan(big, 1, P, 1 << 62) == EUNSUPPORTED
+
+
 def test_adamw_plan(lib):
     """The plan covers every tensor once, whatever their sizes, and tensors of no elements cost nothing."""
     assert lib.adamw_plan_bytes(None, 0) == 0 and lib.adamw_plan(None, 0, None, 0) == OK
