@@ -8,7 +8,8 @@
 // ties go to the lowest expert whatever the lanes do. Selection compares the logits themselves, never
 // rounded probabilities.
 //
-// Ordering. A stable counting sort without atomics on the result: workgroup b (128 tokens, or more so that there are at most 256) counts
+// Ordering. A stable counting sort without atomics on the result: workgroup b (128 tokens, or more, so that there are
+// at most 256 workgroups) counts
 // its pairs per expert into row b of a table in ws; the second launch adds up the rows before its own for
 // the start of its pairs of each expert, and numbers its pairs in order, 64 at a time in a wave (a pair's
 // rank among the lanes of its expert comes from one ballot for each bit of the expert's index). Up to
