@@ -16,8 +16,8 @@
 //  * one barrier a k-step (a slab, where both operands have k contiguous: one of them then has three slots, so that
 //    their loads take turns; all in one k-step, the loads themselves waited for their place), at which the wave's next
 //    products already have their operands in registers.
-// Measured, 16384 tokens, k = 2, 8 experts of 4096 x 4096: forward 786 to 821 us, Delta_X and Delta_W together 1635 to
-// 1710 (1.3 to 1.4 PFLOP/s; a library product of 8192 x 4096 x 4096 reaches 1.56). The matrix cores are busy 68 to 72%
+// Measured, 16384 tokens, k = 2, 8 experts of 4096 x 4096: forward 786 to 849 us, Delta_X and Delta_W together 1635 to
+// 1728 (1.3 to 1.4 PFLOP/s; a library product of 8192 x 4096 x 4096 reaches 1.56). The matrix cores are busy 68 to 72%
 // of the cycles; the rest is the last, partial round of tiles and the start and end of each.
 //
 // Slabs in LDS. An operand with k contiguous: rows of 128 bytes, the 16-byte chunks XORed with row%8. By k-rows:
