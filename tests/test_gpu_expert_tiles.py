@@ -1,6 +1,6 @@
 """The products of any size on each of their tiles, at sizes that the rule of csrc/expert_tile.hip sends there.
 
-Against 64 bits with the bounds of test_gpu_expert.py, whose own sizes all take tiles of 64 x 32.
+Against 64 bits with the bounds of test_gpu_expert.py, whose own sizes all take tiles of 64 x 32."""
 import pytest
 
 from test_gpu_expert import Layer, _check_bwd, _check_fwd
