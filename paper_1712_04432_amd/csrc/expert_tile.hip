@@ -95,12 +95,11 @@ struct TrTile {
   static constexpr int VEC = 16 / (int)sizeof(T);
   static constexpr int NB = 8 * R / VEC;
   u32x4 v[SETS][VEC];
-  int col, by;  // this thread's first column of the matrix
+  int col, first;  // first column of the matrix that this thread reads; that is its own
   __device__ __forceinline__ static int first_k(int tid) { return (tid & 7) * VEC; }
   __device__ __forceinline__ void init(int col0, int width, int tid) {
-    const int c = col0 + (tid >> 3) * VEC;
-    col = width >= VEC ? min(c, width - VEC) : c;  // (narrower matrices: load_edge)
-    by = min(c - col, VEC);
+    first = col0 + (tid >> 3) * VEC;
+    col = width >= VEC ? min(first, width - VEC) : first;  // (narrower matrices: load_edge)
   }
   // element by element. krow(j): the first element of the thread's k-row j, or null for zeros
   template <typename F>
@@ -136,6 +135,7 @@ struct TrTile {
   }
   __device__ __forceinline__ void store(int set, char *lds, int tid) {
     if (tid >= NB) return;
+    const int by = first - col;
 #pragma unroll
     for (int r = 0; r < VEC; ++r) {
       u32x4 o;
@@ -160,8 +160,9 @@ __device__ __forceinline__ bool positive(T v) {
   else return v > 0.f;
 }
 
-// TM, TN: columns (m) and rows (n) of a tile.
-template <typename T, int PASS, int TM, int TN>
+// TM, TN: columns (m) and rows (n) of a tile. GATHER: Delta_W with x's rows by index. (An instance for each way: with both
+// in one, fp32 Delta_W took 141 registers instead of 117 and 127, and three waves a SIMD instead of four.)
+template <typename T, int PASS, int TM, int TN, bool GATHER>
 __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int tiles_m, int tiles_n) {
   constexpr int VEC = 16 / (int)sizeof(T);
   constexpr int BK = 8 * VEC;
@@ -220,13 +221,14 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
   }
   // Delta_W: the rows of x of this thread's k-rows, read a step ahead of their use (read with it, every row's load
   // waited for its index and, loads coming back in order, for all loads before that)
-  int xrow[PASS == EXPERT_DW ? VEC : 1];
+  constexpr bool GATHER_W = PASS == EXPERT_DW && GATHER;
+  int xrow[GATHER_W ? VEC : 1];
   auto next_rows = [&](int k0) {
-    if constexpr (PASS == EXPERT_DW) {
+    if constexpr (GATHER_W) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const int k = k0 + ka0 + j;
-        xrow[j] = k < K ? (a.rows ? a.rows[r0 + k] : r0 + k) : -1;
+        xrow[j] = k < K ? a.rows[r0 + k] : -1;
       }
     }
   };
@@ -248,13 +250,16 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
       wk += BK * a.ldw;
     }
     if constexpr (PASS == EXPERT_DW) {
-      auto x_at = [&](int j) { return xrow[j] >= 0 && xrow[j] < a.n_x ? x + (int64_t)xrow[j] * a.ldx : nullptr; };
+      auto x_at = [&](int j) -> const T * {
+        if constexpr (GATHER) return (uint32_t)xrow[j] < (uint32_t)a.n_x ? x + (int64_t)xrow[j] * a.ldx : nullptr;
+        else return k0 + ka0 + j < k_end && a.n_x > 0 ? x + (int64_t)(r0 + k0 + ka0 + j) * a.ldx : nullptr;
+      };
       auto y_at = [&](int j) { return k0 + kb0 + j < k_end ? dy + (int64_t)(r0 + k0 + kb0 + j) * a.lddy : nullptr; };
       if (!inside) {
         ta.load_edge(set, x_at, M, tid);
         tb.load_edge(set, y_at, n_end, tid_b);
       } else {
-        if (!G && !a.rows) ta.load_rows(set, xk, a.ldx, tid);
+        if constexpr (!G && !GATHER) ta.load_rows(set, xk, a.ldx, tid);
         else ta.load_each(set, x_at, x, tid);
         if (!G) tb.load_rows(set, yk, a.lddy, tid_b);
         else tb.load_each(set, y_at, dy, tid_b);
@@ -432,9 +437,10 @@ static int launch(int pass, const ExpertArgs &a, hipStream_t s) {
   const int cm = (int)tm, cn = (int)tn;
   {
     LaunchTimer t(IMBD_K_EXPERT_FWD + pass, 0, s);
-    if (pass == EXPERT_FWD) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_FWD, TM, TN>), grid, wg, 0, s, a, cm, cn);
-    else if (pass == EXPERT_DX) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DX, TM, TN>), grid, wg, 0, s, a, cm, cn);
-    else hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DW, TM, TN>), grid, wg, 0, s, a, cm, cn);
+    if (pass == EXPERT_FWD) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_FWD, TM, TN, false>), grid, wg, 0, s, a, cm, cn);
+    else if (pass == EXPERT_DX) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DX, TM, TN, false>), grid, wg, 0, s, a, cm, cn);
+    else if (a.rows) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DW, TM, TN, true>), grid, wg, 0, s, a, cm, cn);
+    else hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DW, TM, TN, false>), grid, wg, 0, s, a, cm, cn);
   }
   return check_launch("expert_tile");
 }
