@@ -329,3 +329,76 @@ def test_refusals(imbd, dev):
         imbd.AdamW([{**t, "decay": -1.0}])
     imbd.adamw_step(imbd.AdamW([]), lr=1e-3)
     torch.cuda.synchronize()
+
+
+class _Beside:
+    """The binding, its plans with one more tensor."""
+
+    def __init__(self, imbd, other):
+        self.imbd, self.other, self.plan = imbd, other, None
+
+    def AdamW(self, tensors):
+        self.plan = self.imbd.AdamW([self.other, *tensors])
+        return self.plan
+
+    def adamw_step(self, *args, **kw):
+        return self.imbd.adamw_step(*args, **kw)
+
+
+# the plan's flags of a tensor, and what adamw_write_plan compares with 512 MiB: every array of the set once
+GRAD_BF16, STATE8, VECTOR, STREAM = 1, 2, 4, 8
+RECORD, FLAGS_AT = 72, 68
+
+
+def _footprint(t):
+    each = sum(t[k].element_size() for k in ("w", "grad", "m", "v"))
+    return t["w"].numel() * (each + (2 if t.get("w_lp") is not None else 0))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+def test_steps_past_the_caches(imbd, dev, bits, grad):
+    """Every form of the update that loads and stores past the caches against the formulas in 64 bits, and its bits
+    against those of a small set. (A test of the set's size and of the plan's flags: these forms have run.)"""
+    import torch
+    n = 40_000_000
+    big = {k: torch.zeros(n, device=dev, dtype=dt) for k, dt in
+           (("w", torch.float32), ("w_lp", torch.bfloat16), ("grad", torch.float32), ("m", torch.float32), ("v", torch.float32))}
+    assert _footprint(big) > 600 << 20
+    beside = _Beside(imbd, big)
+    pairs = _tensors(dev, SIZES, bits, grad, seed=18)
+    alone = [t for t, _ in _tensors(dev, SIZES, bits, grad, seed=18)]
+    assert sum(_footprint(t) for t in alone) < 64 << 20
+    small = imbd.AdamW(alone)
+    for step in (1, 2, 1000):
+        _check_step(beside, pairs, step)
+        imbd.adamw_step(small, step=step, **HYPER)
+    flags = [int.from_bytes(bytes(beside.plan.plan[i * RECORD + FLAGS_AT:][:4].tolist()), "little") for i in range(len(SIZES) + 1)]
+    want = VECTOR | STREAM | (STATE8 if bits == 8 else 0) | (GRAD_BF16 if grad == "bf16" else 0)
+    assert flags == [VECTOR | STREAM] + [want] * len(SIZES)
+    assert not int.from_bytes(bytes(small.plan[FLAGS_AT:][:4].tolist()), "little") & STREAM
+    for (x, _), y in zip(pairs, alone):
+        for k in x:
+            if k != "decay":
+                assert torch.equal(x[k].view(torch.uint8), y[k].view(torch.uint8)), k
+    assert not big["w"].any() and not big["m"].any() and not big["v"].any() and not big["w_lp"].any()
+
+
+def test_a_large_tensor_past_the_caches(imbd, dev):
+    """A tensor that is itself past the caches, to its last element: 8 million against the formulas, the others still."""
+    import torch
+    n = 36_000_003
+    big = {k: torch.zeros(n, device=dev, dtype=dt) for k, dt in
+           (("w", torch.float32), ("grad", torch.float32), ("m", torch.float32), ("v", torch.float32))}
+    assert _footprint(big) > 512 << 20
+    (t, _), = _tensors(dev, [8_000_003], 32, "f32", 19)
+    tail = {k: v[n - 8_000_003:] for k, v in big.items()}
+    for k in tail:
+        tail[k].copy_(t[k])
+    old = {k: v.clone() for k, v in tail.items()}
+    imbd.adamw_step(imbd.AdamW([big]), step=4, **HYPER)
+    w, m, v, msize, usize = _ref({**old, "decay": 0.0}, 4, **HYPER)
+    e = 2.0 ** -24
+    assert ((tail["w"].double() - w).abs() <= 16 * e * usize + 3 * e * (w.abs() + old["w"].double().abs())).all()
+    assert ((tail["m"].double() - m).abs() <= 4 * e * msize).all() and ((tail["v"].double() - v).abs() <= 6 * e * v).all()
+    assert not any(big[k][:n - 8_000_003].any() for k in big)
