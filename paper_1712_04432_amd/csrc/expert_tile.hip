@@ -422,12 +422,12 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
 
 }  // namespace
 
-template <typename T, int TM, int TN>
-static int launch(int pass, const ExpertArgs &a, hipStream_t s) {
-  const int M = pass == EXPERT_FWD ? a.d_out : a.d_in;
-  const int64_t tm = pass == EXPERT_DW && !a.out ? 1 : (M + TM - 1) / TM;  // (db alone: the first column of tiles)
+template <typename T, int PASS, int TM, int TN>
+static int launch(const ExpertArgs &a, hipStream_t s) {
+  const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in;
+  const int64_t tm = PASS == EXPERT_DW && !a.out ? 1 : (M + TM - 1) / TM;  // (db alone: the first column of tiles)
   const int64_t tn = (a.d_out + TN - 1) / TN;
-  const int64_t blocks = (pass == EXPERT_DW ? a.E * tn : row_tiles_most(a.n_rows, a.E, TN)) * tm;
+  const int64_t blocks = (PASS == EXPERT_DW ? a.E * tn : row_tiles_most(a.n_rows, a.E, TN)) * tm;
   if (blocks > WORKGROUPS_MOST - 255) {
     set_error("expert product: %lld tiles are more than one launch takes", (long long)blocks);
     return IMBD_EUNSUPPORTED;
@@ -436,35 +436,40 @@ static int launch(int pass, const ExpertArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)((blocks + 255) / 256 * 256)), wg(256);
   const int cm = (int)tm, cn = (int)tn;
   {
-    LaunchTimer t(IMBD_K_EXPERT_FWD + pass, 0, s);
-    if (pass == EXPERT_FWD) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_FWD, TM, TN, false>), grid, wg, 0, s, a, cm, cn);
-    else if (pass == EXPERT_DX) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DX, TM, TN, false>), grid, wg, 0, s, a, cm, cn);
-    else if (a.rows) hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DW, TM, TN, true>), grid, wg, 0, s, a, cm, cn);
-    else hipLaunchKernelGGL((expert_tile_kernel<T, EXPERT_DW, TM, TN, false>), grid, wg, 0, s, a, cm, cn);
+    LaunchTimer t(IMBD_K_EXPERT_FWD + PASS, 0, s);
+    if (PASS == EXPERT_DW && a.rows)
+      hipLaunchKernelGGL((expert_tile_kernel<T, PASS, TM, TN, PASS == EXPERT_DW>), grid, wg, 0, s, a, cm, cn);
+    else
+      hipLaunchKernelGGL((expert_tile_kernel<T, PASS, TM, TN, false>), grid, wg, 0, s, a, cm, cn);
   }
   return check_launch("expert_tile");
 }
 
-template <typename T>
-static int launch_sized(int pass, const ExpertArgs &a, hipStream_t s) {
-  // The largest tile that gives every CU two (128 x 64) or four (64 x 64) workgroups: a large one reads its operands
+template <typename T, int PASS>
+static int launch_sized(const ExpertArgs &a, hipStream_t s) {
+  // The larger tile, 128 x 64 or 64 x 64, where it gives every CU two or four workgroups: a large one reads its operands
   // less often, small ones come out more even and hide each other's waits. bf16, 16384 rows, 8 experts of 2047 x 2049:
   // forward 346 us on 128 x 64 and 453 on 64 x 64, Delta_X 525 and 808, Delta_W 631 and 849; 4096 rows, 1031 x 1037: 47
-  // and 42, 69 and 85, 63 and 76. fp32 forward and Delta_W stay on the smaller (those two sizes: forward 1320 and 1345,
+  // and 42, 69 and 85, 63 and 76. fp32 forward and Delta_W are faster on 64 x 64 (those two sizes: forward 1320 and 1345,
   // 139 and 118); fp32 Delta_X is the better one way or the other by the last round of workgroups (1557 and 1592, 178 and
   // 152, 6400 rows of 1031 x 1037 183 and 202). 3000 rows, 13 experts of 517 x 1023, fp32 forward 54 us on 64 x 32, 74 on 64 x 64.
-  const int M = pass == EXPERT_FWD ? a.d_out : a.d_in;
-  auto tiles = [&](int side) {
-    const int64_t rows = pass == EXPERT_DW ? (int64_t)a.E * ((a.d_out + side - 1) / side)
-                                           : (int64_t)a.n_rows / side + (a.n_rows < a.E ? a.n_rows : a.E) / 2;
-    return rows * ((M + side - 1) / side);
-  };
-  if ((sizeof(T) == 2 || pass == EXPERT_DX) && tiles(128) >= 256) return launch<T, 128, 64>(pass, a, s);
-  return tiles(64) >= 1024 ? launch<T, 64, 64>(pass, a, s) : launch<T, 64, 32>(pass, a, s);
+  constexpr int SIDE = sizeof(T) == 2 || PASS == EXPERT_DX ? 128 : 64;
+  const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in;
+  const int64_t rows = PASS == EXPERT_DW ? (int64_t)a.E * ((a.d_out + SIDE - 1) / SIDE)
+                                         : (int64_t)a.n_rows / SIDE + (a.n_rows < a.E ? a.n_rows : a.E) / 2;
+  const int64_t squares = rows * ((M + SIDE - 1) / SIDE);
+  return squares >= (SIDE == 128 ? 256 : 1024) ? launch<T, PASS, SIDE, 64>(a, s) : launch<T, PASS, 64, 32>(a, s);
+}
+
+template <typename T>
+static int launch_pass(int pass, const ExpertArgs &a, hipStream_t s) {
+  return pass == EXPERT_FWD  ? launch_sized<T, EXPERT_FWD>(a, s)
+         : pass == EXPERT_DX ? launch_sized<T, EXPERT_DX>(a, s)
+                             : launch_sized<T, EXPERT_DW>(a, s);
 }
 
 int run_expert_tile(int pass, int dtype, const ExpertArgs &a, hipStream_t s) {
-  return dtype == IMBD_BF16 ? launch_sized<uint16_t>(pass, a, s) : launch_sized<float>(pass, a, s);
+  return dtype == IMBD_BF16 ? launch_pass<uint16_t>(pass, a, s) : launch_pass<float>(pass, a, s);
 }
 
 }  // namespace imbd

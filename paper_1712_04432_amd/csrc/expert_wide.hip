@@ -158,8 +158,8 @@ constexpr int xw_lds_bytes() {
 }
 
 // ES: bytes of an output (a kernel for each: with both in one, the sums were copied ahead of the branch, and spilled)
-template <int PASS, int BM, int BN, bool GATHER, int ES, int WGS>
-__global__ void __launch_bounds__(256, WGS) expert_wide_kernel(ExpertArgs a, int tiles_m, int tiles_n) {
+template <int PASS, int BM, int BN, bool GATHER, int ES>
+__global__ void __launch_bounds__(256, 1) expert_wide_kernel(ExpertArgs a, int tiles_m, int tiles_n) {
   using Sh = Shape<PASS, BM, BN>;
   constexpr bool A_KC = Sh::A_KC, B_KC = Sh::B_KC;
   constexpr int FM = Sh::FM, FN = Sh::FN;
@@ -654,7 +654,7 @@ bool expert_wide_fits(int pass, int dtype, const ExpertArgs &a) {
   return a.n_rows < (1 << 29);  // byte offsets into rows
 }
 
-template <int PASS, int BM, int BN, int ES, int WGS>
+template <int PASS, int BM, int BN, int ES>
 static int launch(const ExpertArgs &a, hipStream_t s) {
   const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in;
   const int64_t tm = PASS == EXPERT_DW && !a.out ? 1 : (M + BM - 1) / BM;
@@ -669,10 +669,10 @@ static int launch(const ExpertArgs &a, hipStream_t s) {
   {
     LaunchTimer t(IMBD_K_EXPERT_FWD + PASS, 0, s);
     if (a.rows && PASS != EXPERT_DX)  // (Delta_X gathers nothing but its mask)
-      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, PASS != EXPERT_DX, ES, WGS>), grid, dim3(256), 0, s, a, (int)tm,
+      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, PASS != EXPERT_DX, ES>), grid, dim3(256), 0, s, a, (int)tm,
                          tiles_n);
     else
-      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, false, ES, WGS>), grid, dim3(256), 0, s, a, (int)tm, tiles_n);
+      hipLaunchKernelGGL((expert_wide_kernel<PASS, BM, BN, false, ES>), grid, dim3(256), 0, s, a, (int)tm, tiles_n);
   }
   return check_launch("expert_wide");
 }
@@ -694,14 +694,14 @@ static int launch_rows(const ExpertArgs &a, hipStream_t s) {
   const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in, K = PASS == EXPERT_FWD ? a.d_in : a.d_out;
   const bool half = a.out_dtype == IMBD_BF16;
   if (row_tile(a, (M + 255) / 256, K) == 128)
-    return half ? launch<PASS, 256, 128, 2, 1>(a, s) : launch<PASS, 256, 128, 4, 1>(a, s);
-  return half ? launch<PASS, 256, 256, 2, 1>(a, s) : launch<PASS, 256, 256, 4, 1>(a, s);
+    return half ? launch<PASS, 256, 128, 2>(a, s) : launch<PASS, 256, 128, 4>(a, s);
+  return half ? launch<PASS, 256, 256, 2>(a, s) : launch<PASS, 256, 256, 4>(a, s);
 }
 
 int run_expert_wide(int pass, const ExpertArgs &a, hipStream_t s) {
   if (pass == EXPERT_FWD) return launch_rows<EXPERT_FWD>(a, s);
   if (pass == EXPERT_DX) return launch_rows<EXPERT_DX>(a, s);
-  return launch<EXPERT_DW, 256, 256, 4, 1>(a, s);
+  return launch<EXPERT_DW, 256, 256, 4>(a, s);
 }
 
 }  // namespace imbd
