@@ -80,11 +80,13 @@ inline int64_t row_tiles_most(int n_rows, int E, int TR) {
   return ((int64_t)n_rows + used * (TR - 1)) / TR;
 }
 
+// The products' launches. check: only whether one launch takes the call (expert_bwd has two, and launches none of a call
+// that it refuses).
 // Any sizes, strides and alignments, fp32 and bf16 (csrc/expert_tile.hip).
-int run_expert_tile(int pass, int dtype, const ExpertArgs &a, hipStream_t s);
+int run_expert_tile(int pass, int dtype, const ExpertArgs &a, bool check, hipStream_t s);
 // bf16, rows of whole 16-byte chunks (csrc/expert_wide.hip): whether it takes the call, and the launch.
 bool expert_wide_fits(int pass, int dtype, const ExpertArgs &a);
-int run_expert_wide(int pass, const ExpertArgs &a, hipStream_t s);
+int run_expert_wide(int pass, const ExpertArgs &a, bool check, hipStream_t s);
 // The forward product of few rows an expert (csrc/expert_few.hip).
 bool expert_few_fits(int pass, int dtype, const ExpertArgs &a);
 int run_expert_few(const ExpertArgs &a, hipStream_t s);

@@ -128,9 +128,9 @@ int check_tensors(const imbd_adamw_tensor *t, int n, size_t *bytes) {
   return IMBD_OK;
 }
 
-int run_product(int pass, int dtype, const ExpertArgs &a, hipStream_t s) {
-  if (expert_few_fits(pass, dtype, a)) return run_expert_few(a, s);
-  return expert_wide_fits(pass, dtype, a) ? run_expert_wide(pass, a, s) : run_expert_tile(pass, dtype, a, s);
+int run_product(int pass, int dtype, const ExpertArgs &a, hipStream_t s, bool check = false) {
+  if (expert_few_fits(pass, dtype, a)) return run_expert_few(a, s);  // (forward only: never with check)
+  return expert_wide_fits(pass, dtype, a) ? run_expert_wide(pass, a, check, s) : run_expert_tile(pass, dtype, a, check, s);
 }
 
 hipStream_t stream_of(void *s) { return reinterpret_cast<hipStream_t>(s); }
@@ -223,20 +223,21 @@ int expert_bwd(int dtype, int E, int d_out, int d_in, int n_rows, int n_x, const
   ExpertArgs a{};
   a.E = E; a.d_out = d_out; a.d_in = d_in; a.n_rows = n_rows; a.n_x = n_x;
   a.dy = dy; a.lddy = lddy; a.rows = rows; a.offsets = offsets; a.ldx = ldx;
+  ExpertArgs g = a;  // the weights' gradient
+  const bool grad = dw || db;
+  g.x = x;
+  if (!dw) g.n_x = 0;  // (db alone: x may be NULL and is not read)
+  g.out = dw; g.ldo = lddw; g.so = sdw; g.out_dtype = IMBD_F32;
+  g.db = db;
   if (dx && n_rows > 0) {
+    if (grad) TRY(run_product(EXPERT_DW, dtype, g, stream_of(stream), true));
     a.w = w; a.ldw = ldw; a.sw = sw;
     a.x = mask_relu ? x : nullptr;
     a.mask = mask_relu != 0;
     a.out = dx; a.ldo = lddx; a.out_dtype = dx_dtype;
     TRY(run_product(EXPERT_DX, dtype, a, stream_of(stream)));
   }
-  if (!dw && !db) return IMBD_OK;
-  a.mask = 0;
-  a.x = x;
-  if (!dw) a.n_x = 0;  // (db alone: x may be NULL and is not read)
-  a.out = dw; a.ldo = lddw; a.so = sdw; a.out_dtype = IMBD_F32;
-  a.db = db;
-  return run_product(EXPERT_DW, dtype, a, stream_of(stream));
+  return grad ? run_product(EXPERT_DW, dtype, g, stream_of(stream)) : IMBD_OK;
 }
 
 int expert_combine(int dtype, int T, int k, int d, int n_rows, const void *ys, int64_t ldys, const int32_t *slots,

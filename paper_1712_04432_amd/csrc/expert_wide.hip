@@ -655,7 +655,7 @@ bool expert_wide_fits(int pass, int dtype, const ExpertArgs &a) {
 }
 
 template <int PASS, int BM, int BN, int ES>
-static int launch(const ExpertArgs &a, hipStream_t s) {
+static int launch(const ExpertArgs &a, bool check, hipStream_t s) {
   const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in;
   const int64_t tm = PASS == EXPERT_DW && !a.out ? 1 : (M + BM - 1) / BM;
   const int64_t tn = (a.d_out + BN - 1) / BN;
@@ -664,6 +664,7 @@ static int launch(const ExpertArgs &a, hipStream_t s) {
     set_error("expert product: %lld tiles are more than one launch takes", (long long)blocks);
     return IMBD_EUNSUPPORTED;
   }
+  if (check) return IMBD_OK;
   const dim3 grid((unsigned)((blocks + 255) / 256 * 256));
   const int tiles_n = (int)(PASS == EXPERT_DW ? tn : rows);
   {
@@ -690,18 +691,18 @@ static int row_tile(const ExpertArgs &a, int tm, int K) {
 }
 
 template <int PASS>
-static int launch_rows(const ExpertArgs &a, hipStream_t s) {
+static int launch_rows(const ExpertArgs &a, bool check, hipStream_t s) {
   const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in, K = PASS == EXPERT_FWD ? a.d_in : a.d_out;
   const bool half = a.out_dtype == IMBD_BF16;
   if (row_tile(a, (M + 255) / 256, K) == 128)
-    return half ? launch<PASS, 256, 128, 2>(a, s) : launch<PASS, 256, 128, 4>(a, s);
-  return half ? launch<PASS, 256, 256, 2>(a, s) : launch<PASS, 256, 256, 4>(a, s);
+    return half ? launch<PASS, 256, 128, 2>(a, check, s) : launch<PASS, 256, 128, 4>(a, check, s);
+  return half ? launch<PASS, 256, 256, 2>(a, check, s) : launch<PASS, 256, 256, 4>(a, check, s);
 }
 
-int run_expert_wide(int pass, const ExpertArgs &a, hipStream_t s) {
-  if (pass == EXPERT_FWD) return launch_rows<EXPERT_FWD>(a, s);
-  if (pass == EXPERT_DX) return launch_rows<EXPERT_DX>(a, s);
-  return launch<EXPERT_DW, 256, 256, 4>(a, s);
+int run_expert_wide(int pass, const ExpertArgs &a, bool check, hipStream_t s) {
+  if (pass == EXPERT_FWD) return launch_rows<EXPERT_FWD>(a, check, s);
+  if (pass == EXPERT_DX) return launch_rows<EXPERT_DX>(a, check, s);
+  return launch<EXPERT_DW, 256, 256, 4>(a, check, s);
 }
 
 }  // namespace imbd

@@ -181,3 +181,12 @@ def test_adamw_step_refuses(lib, bad):
     a.update(bad)
     assert lib.adamw_step(*a.values(), None) == EINVAL
     assert lib.adamw_step(None, 0, 0, 0.1, 0.9, 0.99, 1e-8, 1.0, 1, None, None) == OK
+
+
+@pytest.mark.parametrize("dtype,d_in", [(0, 8), (1, 33)])
+def test_bwd_launches_nothing_of_a_call_that_it_refuses(lib, dtype, d_in):
+    """db has more tiles (2^24 of 64 rows) than a launch takes and dx has not: both are looked at before dx is launched,
+    which without a device would be another error."""
+    a = {**BWD, "dtype": dtype, "dx_dtype": dtype, "E": 1, "d_out": 2 ** 30, "d_in": d_in, "n_rows": 1, "n_x": 1,
+         "rows": None, "ldw": d_in, "ldx": d_in, "lddx": d_in, "lddy": 2 ** 30, "mask_relu": 0, "dw": None}
+    assert lib.expert_bwd(*a.values(), None) == EUNSUPPORTED and b"one launch" in lib.imbd_last_error()
