@@ -258,7 +258,8 @@ def conv3x3_tile_bwd(x_pad, w, dy_pad, dw, dx=None, ws=None, stream=None):
 # ------------------------------------------------------------------- a layer of experts
 # These take their sizes from several tensors at once, and the kernels trust them, so the
 # tensors are checked against each other here (ValueError, TypeError); everything else is
-# checked by the library (ImbdError).
+# checked by the library (ImbdError). Sizes reach it as C ints, of which ctypes keeps the low 32 bits:
+# larger ones are refused here too (ValueError).
 def _sizes(t, shape, dtype, name, device, whole=False):
     """Shape, type, device (its index) and layout of one tensor: rows without gaps between elements,
     or (whole) contiguous. Returns its address."""
@@ -280,6 +281,10 @@ def _here(t, name):
     if dev < 0 or dev != _torch()._C._cuda_getDevice():
         raise ValueError(f"{name}: on {t.device}, which is not the current device")
     return dev
+
+
+def _too_large(*sizes):
+    raise ValueError(f"sizes {sizes}: each has to be under 2^31")
 
 
 def _on(stream, device):
@@ -304,6 +309,8 @@ def _float(t, name):
 
 
 def expert_route_workspace_bytes(T: int, E: int, k: int) -> int:
+    if max(T, E, k) >> 31 > 0:
+        _too_large(T, E, k)
     return load().expert_route_workspace_bytes(T, E, k)
 
 
@@ -313,6 +320,8 @@ def expert_route(logits, gates, experts, offsets, rows, slots, ws=None, renorm: 
     lib, dev = load(), _here(logits, "logits")
     T, E = logits.shape
     k = gates.shape[-1]
+    if (T | E | k) >> 31:
+        _too_large(T, E, k)
     i32, f32 = torch.int32, torch.float32
     check(lib.expert_route(T, E, k, bool(renorm), _sizes(logits, (T, E), f32, "logits", dev), _rows_ld(logits),
                            _sizes(gates, (T, k), f32, "gates", dev, True),
@@ -330,6 +339,8 @@ def expert_route_bwd(logits, gates, experts, dgates, dlogits, renorm: bool = Tru
     lib, dev = load(), _here(dlogits, "dlogits")
     T, E = dlogits.shape
     k = gates.shape[-1]
+    if (T | E | k) >> 31:
+        _too_large(T, E, k)
     f32, none = torch.float32, logits is None
     check(lib.expert_route_bwd(T, E, k, bool(renorm), None if none else _sizes(logits, (T, E), f32, "logits", dev),
                                0 if none else _rows_ld(logits), _sizes(gates, (T, k), f32, "gates", dev, True),
@@ -346,6 +357,8 @@ def expert_fwd(w, x, offsets, y, bias=None, relu: bool = False, rows=None, strea
     E, d_out, d_in = w.shape
     (dt, code), (ydt, ycode) = _float(w, "w"), _float(y, "y")
     n, n_x, i32 = y.shape[0], x.shape[0], torch.int32
+    if (E | d_out | d_in | n | n_x) >> 31:
+        _too_large(E, d_out, d_in, n, n_x)
     check(lib.expert_fwd(code, bool(relu), E, d_out, d_in, n, n_x, _sizes(w, (E, d_out, d_in), dt, "w", dev),
                          _rows_ld(w), w.stride(0),
                          None if bias is None else _sizes(bias, (E, d_out), torch.float32, "bias", dev, True),
@@ -364,6 +377,8 @@ def expert_bwd(w, dy, x, offsets, dw=None, db=None, dx=None, rows=None, mask_rel
     dt, code = _float(w, "w")
     n, f32, i32 = dy.shape[0], torch.float32, torch.int32
     n_x = n if x is None else x.shape[0]
+    if (E | d_out | d_in | n | n_x) >> 31:
+        _too_large(E, d_out, d_in, n, n_x)
     dxdt, dxcode = (None, IMBD_F32) if dx is None else _float(dx, "dx")
     check(lib.expert_bwd(code, E, d_out, d_in, n, n_x, _sizes(w, (E, d_out, d_in), dt, "w", dev), _rows_ld(w),
                          w.stride(0), _sizes(dy, (n, d_out), dt, "dy", dev), _rows_ld(dy),
@@ -383,6 +398,8 @@ def expert_combine(ys, slots, y, gates=None, stream=None):
     lib, dev = load(), _here(ys, "ys")
     n, d = ys.shape
     T, k = slots.shape
+    if (T | k | n | d) >> 31:
+        _too_large(T, k, n, d)
     (dt, code), (ydt, ycode) = _float(ys, "ys"), _float(y, "y")
     check(lib.expert_combine(code, T, k, d, n, _sizes(ys, (n, d), dt, "ys", dev), _rows_ld(ys),
                              _sizes(slots, (T, k), torch.int32, "slots", dev, True),
@@ -398,6 +415,8 @@ def expert_combine_bwd(dy, ys, slots, gates, dys, dgates=None, stream=None):
     lib, dev = load(), _here(dy, "dy")
     T, d = dy.shape
     n, k = dys.shape[0], slots.shape[-1]
+    if (T | k | n | d) >> 31:
+        _too_large(T, k, n, d)
     dt, code = _float(dy, "dy")
     f32 = torch.float32
     check(lib.expert_combine_bwd(code, T, k, d, n, _sizes(dy, (T, d), dt, "dy", dev), _rows_ld(dy),
@@ -461,9 +480,11 @@ def adamw_step(plan: AdamW, lr: float, beta1: float = 0.9, beta2: float = 0.999,
     tensor that holds it (read by the kernel, so a captured launch follows it)."""
     lib, torch = load(), _torch()
     dev = plan.device
+    dev_step = None
+    if isinstance(step, int) and step >> 31 > 0:
+        raise ValueError(f"step {step}: has to be under 2^31")
     if dev != torch._C._cuda_getDevice():
         raise ValueError(f"plan: on cuda:{dev}, which is not the current device")
-    dev_step = None
     if not isinstance(step, int):
         dev_step = _sizes(step, step.shape, torch.int32, "step", dev, True)
         if step.numel() != 1:

@@ -190,3 +190,68 @@ def test_bwd_launches_nothing_of_a_call_that_it_refuses(lib, dtype, d_in):
     a = {**BWD, "dtype": dtype, "dx_dtype": dtype, "E": 1, "d_out": 2 ** 30, "d_in": d_in, "n_rows": 1, "n_x": 1,
          "rows": None, "ldw": d_in, "ldx": d_in, "lddx": d_in, "lddy": 2 ** 30, "mask_relu": 0, "dw": None}
     assert lib.expert_bwd(*a.values(), None) == EUNSUPPORTED and b"one launch" in lib.imbd_last_error()
+
+
+class _Fake:
+    """A tensor's description without memory: for calls that are refused before they reach the library."""
+
+    def __init__(self, shape, dtype):
+        import torch
+        self.shape, self.dtype, self.device = torch.Size(shape), dtype, "cuda:0"
+
+    def get_device(self):
+        return 0
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 256
+
+    def numel(self):
+        return self.shape.numel()
+
+    def stride(self, i=None):
+        s = [1]
+        for d in reversed(self.shape[1:]):
+            s.insert(0, s[0] * d)
+        return tuple(s) if i is None else s[i]
+
+
+@pytest.mark.parametrize("size", [2 ** 31, 2 ** 32])
+def test_sizes_past_a_c_int_are_refused(lib, monkeypatch, size):
+    """(As the low 32 bits of 2^32 they would be no rows at all: calls that do nothing and succeed.)"""
+    import torch
+    import types
+    import paper_1712_04432_amd as m
+    monkeypatch.setattr(m, "_here", lambda t, name: 0)
+    monkeypatch.setattr(m, "_on", lambda stream, device: None)
+
+    def b(*s):
+        return _Fake(s, torch.bfloat16)
+
+    def f(*s):
+        return _Fake(s, torch.float32)
+
+    def i(*s):
+        return _Fake(s, torch.int32)
+
+    B = size
+    calls = [lambda: m.expert_route(f(B, 8), f(B, 2), i(B, 2), i(9), i(2 * B), i(B, 2)),
+             lambda: m.expert_route(f(4, B), f(4, 2), i(4, 2), i(B + 1), i(8), i(4, 2)),
+             lambda: m.expert_route_bwd(None, f(B, 2), i(B, 2), f(B, 2), f(B, 8)),
+             lambda: m.expert_route_workspace_bytes(B, 8, 2),
+             lambda: m.expert_fwd(b(2, 8, 8), b(B, 8), i(3), b(B, 8)),
+             lambda: m.expert_fwd(b(2, 8, 8), b(B, 8), i(3), b(4, 8), rows=i(4)),
+             lambda: m.expert_fwd(b(2, B, 8), b(4, 8), i(3), b(4, B)),
+             lambda: m.expert_bwd(b(2, 8, 8), b(B, 8), b(B, 8), i(3), dx=b(B, 8)),
+             lambda: m.expert_bwd(b(2, 8, B), b(4, 8), b(4, B), i(3), dw=f(2, 8, B)),
+             lambda: m.expert_combine(b(4, 8), i(B, 2), b(B, 8)),
+             lambda: m.expert_combine(b(B, 8), i(4, 2), b(4, 8)),
+             lambda: m.expert_combine_bwd(b(B, 8), b(4, 8), i(B, 2), f(B, 2), b(4, 8), f(B, 2)),
+             lambda: m.expert_combine_bwd(b(4, 8), b(B, 8), i(4, 2), f(4, 2), b(B, 8), f(4, 2)),
+             lambda: m.adamw_step(types.SimpleNamespace(device=0), lr=0.1, step=size + 1)]
+    for n, call in enumerate(calls):
+        with pytest.raises(ValueError, match="under 2"):
+            call()
+            pytest.fail(f"call {n}")
