@@ -283,6 +283,9 @@ int adamw_step(const void *plan, size_t plan_bytes, int n_tensors, double lr, do
   if (!std::isfinite(lr) || !std::isfinite(grad_scale)) FAIL(IMBD_EINVAL, "lr and grad_scale must be finite");
   if (!(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1)) FAIL(IMBD_EINVAL, "betas must lie in [0, 1)");
   if (!(eps >= 0) || !std::isfinite(eps)) FAIL(IMBD_EINVAL, "eps must be finite and >= 0");
+  // what the kernel takes in fp32: 0 / 0 and 0 * infinity where an element has no gradient
+  if (eps > 0 && (float)eps == 0.f) FAIL(IMBD_EINVAL, "eps = %g is zero in fp32", eps);
+  if (!std::isfinite((float)(lr / (1 - beta1)))) FAIL(IMBD_EINVAL, "lr / (1 - beta1) = %g overflows fp32", lr / (1 - beta1));
   if (!step_dev && step < 1) FAIL(IMBD_EINVAL, "step = %d, need >= 1", step);
   if (plan_bytes == 0) return IMBD_OK;
   if (!plan || (uintptr_t)plan % 16) FAIL(IMBD_EINVAL, "plan must be set and 16-byte aligned");

@@ -255,3 +255,13 @@ def test_sizes_past_a_c_int_are_refused(lib, monkeypatch, size):
         with pytest.raises(ValueError, match="under 2"):
             call()
             pytest.fail(f"call {n}")
+
+
+@pytest.mark.parametrize("bad", [dict(eps=1e-46), dict(eps=1e-60), dict(lr=1e39), dict(lr=-1e300), dict(lr=1e38, b1=0.99)])
+def test_adamw_step_refuses_what_fp32_does_not_hold(lib, bad):
+    """An eps that fp32 makes zero (an element without gradients would be 0 / 0), a rate lr / (1 - beta1) that it makes
+    infinite (0 * infinity)."""
+    a = dict(plan=None, size=0, n=0, lr=0.1, b1=0.9, b2=0.99, eps=1e-8, gs=1.0, step=1, dev=None)
+    for ok in ({}, dict(eps=0.0), dict(eps=1e-44), dict(lr=1e37, b1=0.0)):
+        assert lib.adamw_step(*{**a, **ok}.values(), None) == OK
+    assert lib.adamw_step(*{**a, **bad}.values(), None) == EINVAL and lib.imbd_last_error()
