@@ -274,14 +274,15 @@ size_t adamw_record_bytes() { return sizeof(AwTensor); }
 size_t adamw_entry_bytes() { return sizeof(AwEntry); }
 
 void adamw_write_plan(const imbd_adamw_tensor *tensors, int n_tensors, void *plan) {
-  // What the set reads and writes in a step. Up to twice the 256 MB of the memory-side cache part of it is still
-  // there a step later; past that the loads and stores go past the caches (fp32 state: 16M elements, 448 MB, 74 us,
-  // and 81 past the caches; 64M, 1.8 GB, 353 and 326. 8-bit state: 16M, 192 MB, 52 and 55; 64M, 770 MB, 226 and 211).
+  // The set's footprint, each array once. While much of it is still in the 256 MB of the memory-side cache a step later
+  // it stays in the caches, then the loads and stores go past them. A step in us, in the caches and past them: fp32 state
+  // and gradients with a copy, 256 MiB 68 and 75, 320 MiB 86 and 92, 384 MiB 126 and 111, 512 MiB 169 and 148, 1 GiB 328
+  // and 298; 8-bit state, bf16 gradients, 256 MiB 85 and 84, 320 MiB 107 and 108, 384 MiB 130 and 125, 1 GiB 342 and 325.
   int64_t bytes = 0;
   for (int i = 0; i < n_tensors; ++i)
     bytes += tensors[i].n * (4 + (tensors[i].w_lp ? 2 : 0) + (tensors[i].grad_dtype == IMBD_BF16 ? 2 : 4) +
                              (tensors[i].state_bits == 8 ? 2 : 8));
-  const bool stream = bytes > (int64_t)512 << 20;
+  const bool stream = bytes > (int64_t)336 << 20;
   AwTensor *rec = reinterpret_cast<AwTensor *>(plan);
   AwEntry *en = reinterpret_cast<AwEntry *>(rec + n_tensors);
   for (int i = 0; i < n_tensors; ++i) {

@@ -265,3 +265,19 @@ def test_adamw_step_refuses_what_fp32_does_not_hold(lib, bad):
     for ok in ({}, dict(eps=0.0), dict(eps=1e-44), dict(lr=1e37, b1=0.0)):
         assert lib.adamw_step(*{**a, **ok}.values(), None) == OK
     assert lib.adamw_step(*{**a, **bad}.values(), None) == EINVAL and lib.imbd_last_error()
+
+
+@pytest.mark.parametrize("bits,grad,lp", [(32, 0, 1), (32, 1, 0), (8, 1, 1), (8, 0, 0)])
+def test_adamw_plan_goes_past_the_caches_by_the_sets_footprint(lib, bits, grad, lp):
+    """Every array of the set counted once: up to 320 MiB through the caches, from 352 MiB on past them."""
+    per = 4 + 2 * lp + (2 if grad else 4) + (2 if bits == 8 else 8)
+    for mib, past in ((320, 0), (352, 8)):
+        n = (mib << 20) // per // 2  # (two tensors)
+        at = [dict(w=(1 << 44) + (i << 40), w_lp=(1 << 45) + (i << 40) if lp else None, grad=(1 << 46) + (i << 40),
+                   m=(1 << 47) + (i << 40), v=(1 << 48) + (i << 40), m_scale=(1 << 49) + (i << 40),
+                   v_scale=(1 << 50) + (i << 40)) for i in range(2)]
+        arr = _array(*(_tensor(n=n, grad_dtype=grad, state_bits=bits, **a) for a in at))
+        buf = np.zeros(lib.adamw_plan_bytes(arr, 2), np.uint8)
+        assert lib.adamw_plan(arr, 2, buf.ctypes.data, len(buf)) == OK
+        flags = buf[:144].view(np.int32).reshape(2, 18)[:, 17]  # the last word of each record
+        assert (flags & 8 == past).all() and (flags & 3 == grad + (2 if bits == 8 else 0)).all()
