@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(AW_NT) adamw_kernel(AwArgs a) {
 
 }  // namespace
 
-int64_t adamw_chunks(int64_t n) { return (n + AW_CHUNK - 1) / AW_CHUNK; }
+int64_t adamw_chunks(int64_t n) { return n / AW_CHUNK + (n % AW_CHUNK != 0); }
 size_t adamw_record_bytes() { return sizeof(AwTensor); }
 size_t adamw_entry_bytes() { return sizeof(AwEntry); }
 

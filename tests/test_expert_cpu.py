@@ -281,3 +281,9 @@ def test_adamw_plan_goes_past_the_caches_by_the_sets_footprint(lib, bits, grad, 
         assert lib.adamw_plan(arr, 2, buf.ctypes.data, len(buf)) == OK
         flags = buf[:144].view(np.int32).reshape(2, 18)[:, 17]  # the last word of each record
         assert (flags & 8 == past).all() and (flags & 3 == grad + (2 if bits == 8 else 0)).all()
+
+
+@pytest.mark.parametrize("n", [2 ** 63 - 1, 2 ** 63 - 4000, 2 ** 62])
+def test_adamw_plan_refuses_a_number_of_elements_past_64_bits(lib, n):
+    arr = _array(_tensor(n=n))
+    assert lib.adamw_plan_bytes(arr, 1) == 0 and lib.adamw_plan(arr, 1, P, 1 << 20) == EUNSUPPORTED
