@@ -70,7 +70,9 @@ __device__ __forceinline__ float wave_max_bits(uint32_t u) {
   return __builtin_bit_cast(float, u);
 }
 
-// 21 pseudo-random bits of an element's index and the step: two rounds of multiply and xor-shift.
+// 21 pseudo-random bits of an element's index and the step: two rounds of multiply and xor-shift. The two multipliers and
+// the shifts are those that C. Wellons published in 2018 ("Prospecting for Hash Functions") for a mixing of 32 bits with
+// little bias, found by search; the step enters by the golden ratio's 2^32 / 1.618..
 __device__ __forceinline__ uint32_t dither21(uint32_t index, uint32_t step) {
   uint32_t h = index + step * 0x9E3779B9u;
   h = (h ^ (h >> 16)) * 0x7FEB352Du;
