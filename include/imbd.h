@@ -372,8 +372,9 @@ int adamw_plan(const imbd_adamw_tensor *tensors, int n_tensors, void *plan, size
  * max v * (1/57344), rounded up or down by a dither of the element's index and t (a second moment
  * that moves by 1 - beta2 a step would stay where it is if rounded to nearest), and never to zero:
  * what is positive and under the smallest normal number is held as that number (2^-14; where the
- * block's scale itself is 0 in fp32, m and v are 0). The update itself takes m and v before that rounding. A NaN or an infinity in a gradient makes the element's
- * state NaN or infinite, and with 8-bit state its whole block's.
+ * block's scale itself is 0 in fp32, m and v are 0). The update itself takes m and v before that
+ * rounding. A NaN or an infinity in a gradient makes the element's state NaN or infinite, and with
+ * 8-bit state its whole block's.
  * plan_bytes and n_tensors as at adamw_plan; plan_bytes == 0 is a no-op. 0 <= beta < 1, eps >= 0,
  * lr, eps and grad_scale finite, lr / (1 - beta1) finite and an eps above 0 not 0 in fp32 (with eps == 0
  * an element whose v is 0 becomes NaN or infinite, as the formula has it). A step_dev that holds less

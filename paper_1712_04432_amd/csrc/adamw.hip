@@ -7,7 +7,7 @@
 // state and bf16 gradients. The plan in device memory is a record for each tensor and, behind the records,
 // a table of chunks of AW_CHUNK elements of one tensor each; a workgroup takes a chunk, so one launch
 // serves tensors of every size, and the chunk's loads are all in flight before the first is used. 300 tensors, 120M
-// elements: 620 us with fp32 state (5.8 TB/s), 365 with 8-bit state and bf16 gradients (5.3 TB/s).
+// elements: 620 us with fp32 state (5.8 TB/s), 365 to 378 with 8-bit state and bf16 gradients (5.1 to 5.3 TB/s).
 //
 // Every product and sum is rounded by itself (no contraction into fused multiply-adds), so the states are
 // the same bits wherever the formulas are evaluated in fp32 in the order written; 8-bit codes then never

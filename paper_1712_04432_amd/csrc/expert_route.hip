@@ -15,8 +15,9 @@
 // rank among the lanes of its expert comes from one ballot for each bit of the expert's index). Up to
 // 128 tokens one workgroup does both in one launch.
 //
-// Bound by latency: 16384 tokens, 64 experts, k = 8 move 11 MB (2.3 us) and take 7.6 us for the choice, 4.8 for the
-// order and 4.4 for the logits' gradient; 16 tokens, k = 4, 4.8 us in one launch.
+// Bound by latency: 16384 tokens, 64 experts, k = 8 move 11 MB (2.3 us) and take 8.3 us for the choice, 5.1 for the
+// order (both on 128 workgroups, half of the CUs) and 4.7 for the logits' gradient (means of ten launches; the least 7.6,
+// 4.6 and 4.4); 16 tokens, k = 4, 5.0 us in one launch (least 4.8).
 
 #include "expert.h"
 

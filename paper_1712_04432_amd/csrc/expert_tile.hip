@@ -9,16 +9,17 @@
 //
 // A workgroup of four waves owns a 128 x 64, 64 x 64 or 64 x 32 tile of D and walks K in steps of 128 bytes a row,
 // double-buffered in LDS, with the loads of the next two steps (Delta_W, and the largest tile: one) in flight over the
-// products; rows of 144 bytes make every fragment one conflict-free 16-byte read. Operands stored by k-rows are transposed in registers on their way.
+// products; rows of 144 bytes make every fragment one conflict-free 16-byte read. Operands stored by k-rows are
+// transposed in registers on their way.
 // Addresses are 64-bit and loads are 16 bytes at any element alignment, so no size or stride is special. Whole
-// steps load without conditions (rows that do not count from a row that exists); the last step of a K that is
-// no whole number of them, and k-rows at the edge of their matrix, chunk by chunk and element by element.
+// steps load without conditions (rows that do not count from a row that exists, blocks cut by the last column earlier and
+// whole); the last step of a K that is no whole number of them looks at each row, and k-rows of less than 16 bytes are
+// read element by element.
 // fp32 operands run on the fp32 matrix instruction: products and sums are fp32 for both types.
 //
-// Measured, 16384 rows, 8 experts of 2047 x 2049: bf16 forward 403 TFLOP/s, Delta_X 254, Delta_W 203 (111 with gathered
-// rows), fp32 98, 88 and 87; bound by the latency of the steps with two workgroups a CU. bf16 Delta_W needs 230 to 250
-// registers for its two transposes and both ways of reading a row; a form with 120, which read blocks cut by the last
-// column element by element, ran at 237 (160 gathered).
+// Measured, 16384 rows, 8 experts of 2047 x 2049: bf16 forward 402 TFLOP/s, Delta_X 262, Delta_W 218 (116 with gathered
+// rows), fp32 102, 88 and 93 (71); bound by the latency of the steps. The transposes of bf16 take 173 to 219 registers in
+// Delta_W and 174 to 182 in Delta_X, which leaves two workgroups a CU; fp32 has four, on 128 x 64 tiles two.
 
 #include <type_traits>
 
