@@ -1,9 +1,9 @@
 """Python binding of libimbd.so: the gfx950 hot path of integrated model/batch/domain
 parallel SGD (Gholami et al., arXiv:1712.04432).
 
-Functions carry the names of the C ABI in include/imbd.h and only marshal arguments:
-torch tensors supply device pointers and the current HIP stream; every step of the path
-runs in the library's kernels. Missing library -> RuntimeError (no fallback).
+Functions carry the names of the C ABI in include/imbd.h and marshal arguments (those of the
+expert layer and of AdamW also check the tensors against each other): torch tensors supply
+device pointers and the current HIP stream; every step of the path runs in the library's kernels. Missing library -> RuntimeError (no fallback).
 
 bf16 tensors are torch.bfloat16 (the bytes are bf16 bit patterns), fp32 tensors
 torch.float32. Activations are [B][d] (one sample per row, the paper's column-major
@@ -435,7 +435,9 @@ class AdamW:
     tensors: sequence of dicts with w (fp32), grad (fp32 or bf16), m and v, and optionally w_lp
     (bf16 copy) and decay (0). 32-bit state: m and v fp32. 8-bit state: m torch.float8_e4m3fn, v
     torch.float8_e5m2, and m_scale and v_scale, fp32 [ceil(n/256)]. All contiguous, of one device,
-    and kept alive by the plan; no two may share memory. Zeros are the state before the first step.
+    and kept alive by the plan; no two may share memory (gradients may). Zeros are the state before the
+    first step. The plan holds addresses and is built tensor by tensor on the host: for a tensor that
+    is allocated again, a gradient too, it has to be made anew.
     """
 
     def __init__(self, tensors):
