@@ -3,7 +3,8 @@ parallel SGD (Gholami et al., arXiv:1712.04432).
 
 Functions carry the names of the C ABI in include/imbd.h and marshal arguments (those of the
 expert layer and of AdamW also check the tensors against each other): torch tensors supply
-device pointers and the current HIP stream; every step of the path runs in the library's kernels. Missing library -> RuntimeError (no fallback).
+device pointers and the current HIP stream; every step of the path runs in the library's
+kernels. Missing library -> RuntimeError (no fallback).
 
 bf16 tensors are torch.bfloat16 (the bytes are bf16 bit patterns), fp32 tensors
 torch.float32. Activations are [B][d] (one sample per row, the paper's column-major
