@@ -333,6 +333,58 @@ int expert_combine_bwd(int dtype, int T, int k, int d, int n_rows, const void *d
                        void *dys, int64_t lddys, float *dgates, void *stream);
 
 /* ====================================================================================
+ * What a vocabulary's logits are for, beside softmax_xent: distillation from a teacher, and
+ * the log probabilities of given tokens. B rows (tokens) of V logits, fp32 or bf16, [B][ldz].
+ *
+ * With q the softmax of z / temperature over all V. A logit of -inf rules its token out (q = 0); a
+ * NaN or +inf makes its row's results NaN, as does a row of -inf only (its lse is -inf). Statistics and sums in
+ * fp32, in a fixed order. Sizes (IMBD_EUNSUPPORTED past them): B < 2^24, V <= 2^30, K <= 256, n <= 64.
+ * ws (256-byte aligned): the *_workspace_bytes function's, which is 0 for sizes that the call refuses
+ * and may be 0 for others too (then ws is not read). No output may overlap an input or another output,
+ * but dlogits may be logits itself (same address, leading dimension and type), which then holds
+ * the gradient instead.
+ * ==================================================================================== */
+
+/* Divergence of the student's softmax q from a teacher's, of whose logits K are known in each
+ * row: ids [B][K] their tokens, teacher [B][K] fp32 their values t, both contiguous, in any order.
+ *   p_j = exp(t_j / temperature) / sum over the row's K, or with lse != NULL (fp32 [B], the logsumexp
+ *         of all the teacher's logits / temperature)  exp(t_j / temperature - lse[b])
+ *   row_loss[b] = w_b temperature^2 sum_j p_j (log p_j - log q_{id_j})
+ *   loss        = inv_batch sum_b row_loss[b]
+ *   dlogits[b][v] = inv_batch w_b temperature (q_v sum_j p_j - sum_j [id_j = v] p_j)
+ * w = weight (fp32 [B], NULL: 1). An entry with id < 0 or t = -inf is no entry (rows with fewer than
+ * K); the same id twice counts as the sum of both. A row without entries or with w_b = 0 has
+ * row_loss 0 and a gradient of zeros, whatever its logits hold; one with an id >= V (and w_b != 0)
+ * has NaN in both, and so has the loss. dlogits [B][lddl] in dlogits_dtype, or NULL (loss only). */
+size_t distill_workspace_bytes(int B, int V, int K);
+int distill_xent(int dtype, int B, int V, int K, const void *logits, int64_t ldz, const int32_t *ids,
+                 const float *teacher, const float *lse, const float *weight, float temperature,
+                 float inv_batch, float *loss, float *row_loss, void *dlogits, int64_t lddl,
+                 int dlogits_dtype, void *ws, size_t ws_bytes, void *stream);
+
+/* Of every row: logp [B] = log q_{tokens[b]}, and where they are not NULL entropy [B] = -sum q log q,
+ * lse [B] = log sum exp(z / temperature), and the n largest logits in descending order, ties to the lowest token:
+ * top_ids [B][n] and top_logp [B][n] = log q of them (n == 0: neither). tokens[b] < 0: no
+ * token, logp 0; tokens[b] >= V: logp NaN. Alternatives are chosen by the logits themselves; a token
+ * that is ruled out or whose logit is NaN is none: where fewer than n are left, id -1 and log
+ * probability -inf. All fp32 or int32, contiguous. */
+size_t token_logprobs_workspace_bytes(int B, int V, int n);
+int token_logprobs(int dtype, int B, int V, int n, const void *logits, int64_t ldz, const int32_t *tokens,
+                   float temperature, float *logp, float *entropy, float *lse, int32_t *top_ids,
+                   float *top_logp, void *ws, size_t ws_bytes, void *stream);
+
+/* The logits' gradient from dlogp [B] and dentropy [B] (either may be NULL: zeros), with lse and entropy
+ * as token_logprobs left them for the same logits, tokens and temperature (entropy may be NULL without dentropy):
+ *   dlogits[b][v] = (g_b ([v = tokens[b]] - q_v) - h_b q_v (log q_v + entropy[b])) / temperature
+ * (log q_v is taken from lse, so it is as exact as an fp32 lse is: off by 2^-23 |lse|.)
+ * g_b = dlogp[b], 0 where tokens[b] < 0 (tokens[b] >= V: the row becomes NaN); h = dentropy. A row
+ * with g_b = h_b = 0 becomes zeros, whatever its logits hold. */
+int token_logprobs_bwd(int dtype, int B, int V, const void *logits, int64_t ldz, const int32_t *tokens,
+                       float temperature, const float *lse, const float *entropy, const float *dlogp,
+                       const float *dentropy, void *dlogits, int64_t lddl, int dlogits_dtype,
+                       void *stream);
+
+/* ====================================================================================
  * AdamW over many tensors in one launch: beside sgd_step, for gradients as mlp_bwd
  * (fuse_sgd = 0) and expert_bwd store them.
  * ==================================================================================== */
@@ -434,7 +486,8 @@ enum imbd_kernel_class {
     IMBD_K_SOFTMAX = 4, IMBD_K_BIAS = 5, IMBD_K_SGD = 6, IMBD_K_CAST = 7,
     IMBD_K_CONV_FWD = 8, IMBD_K_CONV_DGRAD = 9, IMBD_K_CONV_WGRAD = 10,
     IMBD_K_EXPERT_FWD = 11, IMBD_K_EXPERT_DX = 12, IMBD_K_EXPERT_DW = 13,
-    IMBD_K_ROUTE = 14, IMBD_K_COMBINE = 15, IMBD_K_ADAMW = 16
+    IMBD_K_ROUTE = 14, IMBD_K_COMBINE = 15, IMBD_K_ADAMW = 16, IMBD_K_DISTILL = 17,
+    IMBD_K_LOGPROBS = 18, IMBD_K_LINEAR = 19
 };
 /* Start recording HIP events around every launch of kernel class `cls` whose layer tag
  * equals `layer` (-1: any layer), up to max_launches launches. Creates the events

@@ -17,7 +17,8 @@ import ctypes
 from ._abi import (IMBD_BF16, IMBD_F32, IMBD_K_BIAS, IMBD_K_CAST, IMBD_K_CONV_DGRAD,  # noqa: F401
                    IMBD_K_CONV_FWD, IMBD_K_CONV_WGRAD, IMBD_K_GEMM_DW, IMBD_K_GEMM_DX,
                    IMBD_K_GEMM_FWD, IMBD_K_SGD, IMBD_K_SOFTMAX, IMBD_K_SPLITK, IMBD_K_EXPERT_FWD,
-                   IMBD_K_EXPERT_DX, IMBD_K_EXPERT_DW, IMBD_K_ROUTE, IMBD_K_COMBINE, IMBD_K_ADAMW, IMBD_OK,
+                   IMBD_K_EXPERT_DX, IMBD_K_EXPERT_DW, IMBD_K_ROUTE, IMBD_K_COMBINE, IMBD_K_ADAMW,
+                   IMBD_K_DISTILL, IMBD_K_LOGPROBS, IMBD_K_LINEAR, IMBD_OK,
                    IMBD_EINVAL, IMBD_EUNSUPPORTED, IMBD_EHIP, IMBD_EWORKSPACE,
                    IMBD_WS_ACT, IMBD_WS_DY, IMBD_WS_LOGITS, IMBD_WS_ROWLOSS, AdamWTensor, ImbdError,
                    Layer, MlpDesc, check, load)
@@ -35,6 +36,7 @@ __all__ = [
     "timing_end",
     "expert_route_workspace_bytes", "expert_route", "expert_route_bwd", "expert_fwd", "expert_bwd",
     "expert_combine", "expert_combine_bwd", "AdamW", "adamw_step",
+    "distill_workspace_bytes", "distill_xent", "token_logprobs_workspace_bytes", "token_logprobs", "token_logprobs_bwd",
     "ws_view", "dtype_code", "set_option", "get_option", "option_name", "options",
 ]
 
@@ -427,6 +429,102 @@ def expert_combine_bwd(dy, ys, slots, gates, dys, dgates=None, stream=None):
                                  _sizes(gates, (T, k), f32, "gates", dev, True), _sizes(dys, (n, d), dt, "dys", dev),
                                  _rows_ld(dys), None if dgates is None else _sizes(dgates, (T, k), f32, "dgates", dev, True),
                                  _on(stream, dev)), "expert_combine_bwd")
+
+
+# ------------------------------------------------- what a vocabulary's logits are for
+# (Checked as the expert layer's tensors are. Logits and their gradient are of the same kind, so
+# that one may take the other's place.)
+def _opt(t, shape, dtype, name, device):
+    """The address of an optional contiguous tensor."""
+    return None if t is None else _sizes(t, shape, dtype, name, device, True)
+
+
+def _ws(ws, device):
+    """Address and bytes of an optional workspace."""
+    return (None, 0) if ws is None else (_sizes(ws, ws.shape, ws.dtype, "ws", device, True),
+                                         ws.numel() * ws.element_size())
+
+
+def _gradient(dlogits, B, V, device):
+    """Address, leading dimension and type of the logits' gradient."""
+    dt, code = _float(dlogits, "dlogits")
+    return _sizes(dlogits, (B, V), dt, "dlogits", device), _rows_ld(dlogits), code
+
+
+def distill_workspace_bytes(B: int, V: int, K: int) -> int:
+    if max(B, V, K) >> 31 > 0:
+        _too_large(B, V, K)
+    return load().distill_workspace_bytes(B, V, K)
+
+
+def distill_xent(logits, ids, teacher, inv_batch: float, loss, row_loss, dlogits=None, temperature: float = 1.0,
+                 lse=None, weight=None, ws=None, stream=None):
+    """Divergence of softmax(logits / temperature) from a teacher's top logits (`teacher` [B][K] of the
+    tokens `ids`), and its gradient (dlogits may be logits)."""
+    torch = _torch()
+    lib, dev = load(), _here(logits, "logits")
+    B, V = logits.shape
+    K = ids.shape[-1]
+    if (B | V | K) >> 31:
+        _too_large(B, V, K)
+    dt, code = _float(logits, "logits")
+    f32 = torch.float32
+    at_dl, lddl, dlcode = (None, 0, code) if dlogits is None else _gradient(dlogits, B, V, dev)
+    at_ws, ws_bytes = _ws(ws, dev)
+    if loss.numel() != 1:
+        raise ValueError(f"loss: {loss.numel()} elements, need 1")
+    check(lib.distill_xent(code, B, V, K, _sizes(logits, (B, V), dt, "logits", dev), _rows_ld(logits),
+                           _sizes(ids, (B, K), torch.int32, "ids", dev, True),
+                           _sizes(teacher, (B, K), f32, "teacher", dev, True), _opt(lse, (B,), f32, "lse", dev),
+                           _opt(weight, (B,), f32, "weight", dev), temperature, inv_batch,
+                           _sizes(loss, loss.shape, f32, "loss", dev), _sizes(row_loss, (B,), f32, "row_loss", dev, True),
+                           at_dl, lddl, dlcode, at_ws, ws_bytes, _on(stream, dev)), "distill_xent")
+
+
+def token_logprobs_workspace_bytes(B: int, V: int, n: int) -> int:
+    if max(B, V, n) >> 31 > 0:
+        _too_large(B, V, n)
+    return load().token_logprobs_workspace_bytes(B, V, n)
+
+
+def token_logprobs(logits, tokens, logp, entropy=None, lse=None, top_ids=None, top_logp=None, temperature: float = 1.0,
+                   ws=None, stream=None):
+    """The log probability of each row's token, the rows' entropy and log-sum-exp, and the
+    top_ids.shape[1] most probable tokens of each."""
+    torch = _torch()
+    lib, dev = load(), _here(logits, "logits")
+    B, V = logits.shape
+    n = 0 if top_ids is None else top_ids.shape[-1]
+    if (B | V | n) >> 31:
+        _too_large(B, V, n)
+    dt, code = _float(logits, "logits")
+    f32 = torch.float32
+    at_ws, ws_bytes = _ws(ws, dev)
+    check(lib.token_logprobs(code, B, V, n, _sizes(logits, (B, V), dt, "logits", dev), _rows_ld(logits),
+                             _sizes(tokens, (B,), torch.int32, "tokens", dev, True), temperature,
+                             _sizes(logp, (B,), f32, "logp", dev, True), _opt(entropy, (B,), f32, "entropy", dev),
+                             _opt(lse, (B,), f32, "lse", dev), _opt(top_ids, (B, n), torch.int32, "top_ids", dev),
+                             _opt(top_logp, (B, n), f32, "top_logp", dev), at_ws, ws_bytes, _on(stream, dev)),
+          "token_logprobs")
+
+
+def token_logprobs_bwd(logits, tokens, lse, dlogits, dlogp=None, entropy=None, dentropy=None, temperature: float = 1.0,
+                       stream=None):
+    """The logits' gradient from those of the log probabilities and of the entropies (dlogits may be
+    logits); lse and entropy as token_logprobs left them."""
+    torch = _torch()
+    lib, dev = load(), _here(logits, "logits")
+    B, V = logits.shape
+    if (B | V) >> 31:
+        _too_large(B, V)
+    dt, code = _float(logits, "logits")
+    f32 = torch.float32
+    at_dl, lddl, dlcode = _gradient(dlogits, B, V, dev)
+    check(lib.token_logprobs_bwd(code, B, V, _sizes(logits, (B, V), dt, "logits", dev), _rows_ld(logits),
+                                 _sizes(tokens, (B,), torch.int32, "tokens", dev, True), temperature,
+                                 _sizes(lse, (B,), f32, "lse", dev, True), _opt(entropy, (B,), f32, "entropy", dev),
+                                 _opt(dlogp, (B,), f32, "dlogp", dev), _opt(dentropy, (B,), f32, "dentropy", dev),
+                                 at_dl, lddl, dlcode, _on(stream, dev)), "token_logprobs_bwd")
 
 
 # ------------------------------------------------------------------------------- AdamW

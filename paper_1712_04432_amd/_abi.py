@@ -18,7 +18,8 @@ IMBD_OPT_COUNT = 15
 IMBD_STATIC_SCRATCH_BYTES = 64 << 20
 (IMBD_K_GEMM_FWD, IMBD_K_GEMM_DX, IMBD_K_GEMM_DW, IMBD_K_SPLITK, IMBD_K_SOFTMAX, IMBD_K_BIAS,
  IMBD_K_SGD, IMBD_K_CAST, IMBD_K_CONV_FWD, IMBD_K_CONV_DGRAD, IMBD_K_CONV_WGRAD, IMBD_K_EXPERT_FWD,
- IMBD_K_EXPERT_DX, IMBD_K_EXPERT_DW, IMBD_K_ROUTE, IMBD_K_COMBINE, IMBD_K_ADAMW) = range(17)
+ IMBD_K_EXPERT_DX, IMBD_K_EXPERT_DW, IMBD_K_ROUTE, IMBD_K_COMBINE, IMBD_K_ADAMW, IMBD_K_DISTILL, IMBD_K_LOGPROBS,
+ IMBD_K_LINEAR) = range(20)
 
 # every function the header declares: name -> (restype, argtypes)
 _i, _l, _p, _f, _d, _z = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_double, ctypes.c_size_t
@@ -72,6 +73,11 @@ SIGNATURES = {
                         _p]),
     "expert_combine": (_i, [_i, _i, _i, _i, _i, _p, _l, _p, _p, _p, _l, _i, _p]),
     "expert_combine_bwd": (_i, [_i, _i, _i, _i, _i, _p, _l, _p, _l, _p, _p, _p, _l, _p, _p]),
+    "distill_workspace_bytes": (_z, [_i, _i, _i]),
+    "distill_xent": (_i, [_i, _i, _i, _i, _p, _l, _p, _p, _p, _p, _f, _f, _p, _p, _p, _l, _i, _p, _z, _p]),
+    "token_logprobs_workspace_bytes": (_z, [_i, _i, _i]),
+    "token_logprobs": (_i, [_i, _i, _i, _i, _p, _l, _p, _f, _p, _p, _p, _p, _p, _p, _z, _p]),
+    "token_logprobs_bwd": (_i, [_i, _i, _i, _p, _l, _p, _f, _p, _p, _p, _p, _p, _l, _i, _p]),
     "adamw_plan_bytes": (_z, [ctypes.POINTER(AdamWTensor), _i]),
     "adamw_plan": (_i, [ctypes.POINTER(AdamWTensor), _i, _p, _z]),
     "adamw_step": (_i, [_p, _z, _i, _d, _d, _d, _d, _f, _i, _p, _p]),

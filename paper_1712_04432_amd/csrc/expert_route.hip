@@ -20,24 +20,13 @@
 // 4.6 and 4.4); 16 tokens, k = 4, 5.0 us in one launch (least 4.8).
 
 #include "expert.h"
+#include "order_key.h"
 
 namespace imbd {
 namespace {
 
 constexpr int RT_NT = 1024;      // threads of a workgroup
 constexpr int RT_BLOCKS = 256;   // workgroups at most (rows of the table)
-
-// Whole number of the same order as v; NaN the largest, 0 is below every value.
-__device__ __forceinline__ uint32_t order_key(float v) {
-  if (v != v) return 0xffffffffu;
-  const uint32_t u = __builtin_bit_cast(uint32_t, v + 0.0f);  // (-0 becomes +0: they tie)
-  return (u >> 31) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ float key_value(uint32_t k) {
-  if (k == 0xffffffffu) return __builtin_nanf("");
-  return __builtin_bit_cast(float, (k >> 31) ? (k & 0x7fffffffu) : ~k);
-}
-constexpr uint32_t KEY_MINUS_INF = 0x007fffffu;  // order_key(-inf)
 
 // The value of the lane that a group's reduction pairs with at distance o: inside 16 lanes by the cross-lane forms
 // of the vector instructions (at 4 and 8 the mirrored lane, which holds the same as its neighbours by then).
