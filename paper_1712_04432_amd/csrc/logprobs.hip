@@ -1,7 +1,14 @@
 // Log probabilities of given tokens, with the entropy and the top alternatives of every row, and their gradient.
 //
-// A workgroup a row. The sums of the softmax are carried in one pass (RowSums in csrc/vocab.h); the alternatives
-// are found one after another, each the largest (logit, lowest token) below the one before.
+// Forward. Bound by reading the logits, once: a workgroup walks a row, or a part of it (row_parts), with the sums of the
+// softmax in registers (RowSums in csrc/vocab.h). A thread's reference m moves only when a group of its logits exceeds
+// it by 16 octaves, so that the sums are rescaled a few times a row and not with every new maximum: fp32 holds 2^16
+// times more than it needs to. Parts are joined in their order by a second launch.
+//
+// Alternatives cost the walk one comparison a chunk: every thread remembers its largest logit's chunk. The n-th largest
+// of 64 disjoint groups' best is a bound that the row's n best reach; the threads whose best reaches it (hardly more than n)
+// have their columns looked at once more, from the caches, and what reaches the bound there is put in order by counting.
+// Where more than fit the list reach it (many equal columns of one thread), the n are found one after another.
 
 #include "order_key.h"
 #include "vocab.h"
@@ -9,8 +16,12 @@
 namespace imbd {
 namespace {
 
+constexpr int LP_NT = 256;     // threads of a workgroup
+constexpr int LP_UNROLL = 4;   // chunks of a thread in flight
+constexpr int LP_LIST = 1024;  // candidates
+
 struct LogprobsArgs {
-  int B, V, n;
+  int V, n, parts, per;
   const void *logits;
   int64_t ldz;
   const int32_t *tokens;
@@ -18,6 +29,8 @@ struct LogprobsArgs {
   float *logp, *entropy, *lse;
   int32_t *top_ids;
   float *top_logp;
+  RowSums *sums;   // more than one part: [b][part]
+  uint64_t *keys;  // ... and the part's n best, in order, [b][part][n]
 };
 
 // A logit and its token as one number: larger logits first, then lower tokens. 0: none.
@@ -26,59 +39,226 @@ __device__ __forceinline__ uint64_t choice_key(float z, int v) {
   if (z != z || k <= KEY_MINUS_INF) return 0;
   return ((uint64_t)k << 32) | (uint32_t)~v;
 }
+__device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-template <typename T>
-__global__ void __launch_bounds__(256) logprobs_kernel(LogprobsArgs a) {
-  __shared__ RowSums part[4];
-  __shared__ uint64_t best[4];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int64_t b = blockIdx.x;
-  const T *z = reinterpret_cast<const T *>(a.logits) + b * a.ldz;
+// The row's results from its sums.
+__device__ __forceinline__ void put_row(const LogprobsArgs &a, int64_t b, const RowSums &r, float zt, int t, float ls) {
+  a.logp[b] = t < 0 ? 0.f : t >= a.V ? __builtin_nanf("") : (zt - r.m) * a.inv_t - ls;
+  if (a.entropy) a.entropy[b] = ls - LN2 * (r.u / r.s);
+  if (a.lse) a.lse[b] = r.m * a.inv_t + ls;
+}
+__device__ __forceinline__ void put_choice(const LogprobsArgs &a, int64_t b, int j, uint64_t key, const RowSums &r, float ls) {
+  a.top_ids[b * a.n + j] = key ? (int)~(uint32_t)key : -1;
+  a.top_logp[b * a.n + j] = key ? (key_value((uint32_t)(key >> 32)) - r.m) * a.inv_t - ls : -INFINITY;
+}
+
+// One workgroup's part of a row. ENT: with u. TOP: remembers where the thread's largest logit is.
+template <typename T, bool ENT, bool TOP>
+__device__ __forceinline__ RowSums walk(const T *z, int cols, float c, float *best, int *best_at) {
+  constexpr int N = chunk_elems<T>();
+  const int tid = threadIdx.x, chunks = (cols + N - 1) / N, whole = cols / N;
+  const float slack = 16.f / c;
   RowSums r{LOWEST, 0.f, 0.f};
-  for (int64_t v = tid; v < a.V; v += 256) {
-    const float x = load_f32(z + v);
-    if (x > r.m) r = moved(r, x, a.c);
-    const float d = scaled(x, r.m, a.c), e = pow2(d);
-    r.s += e;
-    r.u += e * d;
+  auto take = [&](const auto &v, int first) {
+    constexpr int M = sizeof(v) / 16;
+    float top = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < M; ++q) {
+      float cm = chunk_at<T>(v[q], 0);
+#pragma unroll
+      for (int i = 1; i < N; ++i) cm = fmaxf(cm, chunk_at<T>(v[q], i));
+      if constexpr (TOP) {
+        const bool more = cm > *best;
+        *best = more ? cm : *best;
+        *best_at = more ? first + q * LP_NT : *best_at;
+      }
+      top = fmaxf(top, cm);
+    }
+    if (top > r.m + slack) r = moved(r, top, c);
+#pragma unroll
+    for (int q = 0; q < M; ++q) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float x = chunk_at<T>(v[q], i);
+        if constexpr (ENT) {
+          const float d = scaled(x, r.m, c), e = pow2(d);
+          r.s += e;
+          r.u = fmaf(e, d, r.u);
+        } else {
+          r.s += pow2((x - r.m) * c);
+        }
+      }
+    }
+  };
+  int k = tid;
+  for (; k + (LP_UNROLL - 1) * LP_NT < whole; k += LP_UNROLL * LP_NT) {
+    u32x4 v[LP_UNROLL];
+#pragma unroll
+    for (int q = 0; q < LP_UNROLL; ++q) v[q] = load_chunk(z + (int64_t)(k + q * LP_NT) * N);
+    take(v, k);
   }
-  r = wave_joined(r, a.c);
-  if (lane == 0) part[wave] = r;
+  for (; k < chunks; k += LP_NT) {
+    u32x4 v[1];
+    v[0] = k < whole ? load_chunk(z + (int64_t)k * N) : load_cut_chunk(z + (int64_t)k * N, cols - k * N);
+    take(v, k);
+  }
+  return r;
+}
+
+__device__ __forceinline__ RowSums group_joined(RowSums r, float c, RowSums *part) {
+  const int tid = threadIdx.x;
+  r = wave_joined(r, c);
+  if ((tid & 63) == 0) part[tid >> 6] = r;
   __syncthreads();
-  r = joined(joined(part[0], part[1], a.c), joined(part[2], part[3], a.c), a.c);
+  return joined(joined(part[0], part[1], c), joined(part[2], part[3], c), c);
+}
+
+template <typename T, bool ENT, bool TOP>
+__global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobsArgs a) {
+  constexpr int N = chunk_elems<T>(), NW = LP_NT / 64;
+  __shared__ RowSums part[NW];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int64_t b = blockIdx.x / (unsigned)a.parts;
+  const int p = (int)(blockIdx.x - b * a.parts), c0 = p * a.per, cols = min(a.per, a.V - c0);
+  const T *row = reinterpret_cast<const T *>(a.logits) + b * a.ldz, *z = row + c0;
+  int t = -1;
+  float zt = 0.f;
+  if (a.parts == 1 && tid == 0) {
+    t = a.tokens[b];
+    if (t >= 0 && t < a.V) zt = load_f32(row + t);
+  }
+  float best = -INFINITY;
+  int best_at = 0;
+  const RowSums r = group_joined(walk<T, ENT, TOP>(z, cols, a.c, &best, &best_at), a.c, part);
   const float ls = logf(r.s);
   if (tid == 0) {
-    const int t = a.tokens[b];
-    a.logp[b] = t < 0 ? 0.f : t >= a.V ? __builtin_nanf("") : (load_f32(z + t) - r.m) * a.inv_t - ls;
-    if (a.entropy) a.entropy[b] = ls - LN2 * (r.u / r.s);
-    if (a.lse) a.lse[b] = r.m * a.inv_t + ls;
+    if (a.parts == 1) put_row(a, b, r, zt, t, ls);
+    else a.sums[b * a.parts + p] = r;
   }
-  uint64_t last = ~(uint64_t)0;
-  for (int j = 0; j < a.n; ++j) {
-    uint64_t k = 0;
-    for (int64_t v = tid; v < a.V; v += 256) {
-      const uint64_t x = choice_key(load_f32(z + v), (int)v);
-      if (x < last && x > k) k = x;
-    }
+  if constexpr (TOP) {
+    __shared__ uint64_t keys[LP_LIST];
+    __shared__ int threads[LP_NT];
+    __shared__ uint64_t bound_of, next[NW];
+    __shared__ int n_threads, n_keys;
+    auto put = [&](int j, uint64_t key) {
+      if (a.parts == 1) put_choice(a, b, j, key, r, ls);
+      else a.keys[(b * a.parts + p) * a.n + j] = key;
+    };
+    // keys that the thread's best does reach at least, and may reach at most
+    const uint64_t some = choice_key(best, c0 + best_at * N + N - 1), most = choice_key(best, c0 + best_at * N);
+    keys[tid] = some;
+    if (tid == 0) n_threads = n_keys = 0;
+    __syncthreads();
+    if (wave == 0) {
+      uint64_t g = some;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t x = __shfl_xor((unsigned long long)k, o, 64);
-      k = x > k ? x : k;
+      for (int w = 1; w < NW; ++w) g = max64(g, keys[64 * w + lane]);
+      int rank = 0;  // (keys differ, but for 0)
+#pragma unroll
+      for (int i = 0; i < 64; ++i) {
+        const uint64_t k = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(g >> 32), i) << 32) |
+                           (uint32_t)__builtin_amdgcn_readlane((int)g, i);
+        rank += k > g;
+      }
+      const uint64_t at = __ballot(rank == a.n - 1 && g != 0);
+      if (at == 0 && lane == 0) bound_of = 1;  // fewer than n groups have any
+      if (at != 0 && rank == a.n - 1 && g != 0) bound_of = g;
     }
     __syncthreads();
-    if (lane == 0) best[wave] = k;
+    const uint64_t bound = bound_of;
+    if (most >= bound) threads[atomicAdd(&n_threads, 1)] = tid;
     __syncthreads();
-    last = max(max(best[0], best[1]), max(best[2], best[3]));
-    if (tid == 0) {
-      a.top_ids[b * a.n + j] = last ? (int)~(uint32_t)last : -1;
-      a.top_logp[b * a.n + j] = last ? (key_value((uint32_t)(last >> 32)) - r.m) * a.inv_t - ls : -INFINITY;
+    const int chunks = (cols + N - 1) / N;
+    for (int i = wave; i < n_threads; i += NW) {
+      const int owner = threads[i];
+      for (int k = owner + lane * LP_NT; k < chunks; k += 64 * LP_NT) {
+        const T *q = z + (int64_t)k * N;
+        const u32x4 v = (k + 1) * N <= cols ? load_chunk(q) : load_cut_chunk(q, cols - k * N);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const uint64_t key = choice_key(chunk_at<T>(v, j), c0 + k * N + j);
+          if (key >= bound) {
+            const int at = atomicAdd(&n_keys, 1);
+            if (at < LP_LIST) keys[at] = key;
+          }
+        }
+      }
     }
-    if (!last) last = 1;  // (nothing is below it)
+    __syncthreads();
+    const int found = n_keys;
+    if (found <= LP_LIST) {
+      for (int i = tid; i < found; i += LP_NT) {
+        const uint64_t key = keys[i];
+        int rank = 0;
+        for (int j = 0; j < found; ++j) rank += keys[j] > key;
+        if (rank < a.n) put(rank, key);
+      }
+      for (int j = found + tid; j < a.n; j += LP_NT) put(j, 0);
+      return;
+    }
+    uint64_t last = ~(uint64_t)0;
+    for (int j = 0; j < a.n; ++j) {
+      uint64_t k = 0;
+      for (int v = tid; v < cols; v += LP_NT) {
+        const uint64_t x = choice_key(load_f32(z + v), c0 + v);
+        if (x < last) k = max64(k, x);
+      }
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) k = max64(k, __shfl_xor((unsigned long long)k, o, 64));
+      __syncthreads();
+      if (lane == 0) next[wave] = k;
+      __syncthreads();
+      last = max64(max64(next[0], next[1]), max64(next[2], next[3]));
+      if (tid == 0) put(j, last);
+    }
   }
 }
 
+// A row of several parts.
+template <typename T>
+__global__ void __launch_bounds__(LP_NT) logprobs_join_kernel(LogprobsArgs a) {
+  __shared__ uint64_t keys[PARTS_MOST * TOP_MOST];
+  __shared__ int n_keys;
+  const int tid = threadIdx.x;
+  const int64_t b = blockIdx.x;
+  if (tid == 0) n_keys = 0;
+  const int t = a.tokens[b];
+  const float zt = t >= 0 && t < a.V ? load_f32(reinterpret_cast<const T *>(a.logits) + b * a.ldz + t) : 0.f;
+  const RowSums r = joined_parts(a.sums + b * a.parts, a.parts, a.c);
+  const float ls = logf(r.s);
+  if (tid == 0) put_row(a, b, r, zt, t, ls);
+  if (a.n == 0) return;
+  const uint64_t *from = a.keys + b * a.parts * a.n;
+  uint64_t bound = 1;  // the row's n best reach every part's n-th
+  for (int p = 0; p < a.parts; ++p) bound = max64(bound, from[p * a.n + a.n - 1]);
+  __syncthreads();
+  for (int i = tid; i < a.parts * a.n; i += LP_NT)
+    if (from[i] >= bound) keys[atomicAdd(&n_keys, 1)] = from[i];
+  __syncthreads();
+  const int found = n_keys;
+  for (int i = tid; i < found; i += LP_NT) {
+    const uint64_t key = keys[i];
+    int rank = 0;
+    for (int j = 0; j < found; ++j) rank += keys[j] > key;
+    if (rank < a.n) put_choice(a, b, rank, key, r, ls);
+  }
+  for (int j = found + tid; j < a.n; j += LP_NT) put_choice(a, b, j, 0, r, ls);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(LP_NT) row_sums_kernel(LogprobsArgs a) {
+  __shared__ RowSums part[LP_NT / 64];
+  const int64_t b = blockIdx.x / (unsigned)a.parts;
+  const int p = (int)(blockIdx.x - b * a.parts), c0 = p * a.per, cols = min(a.per, a.V - c0);
+  const T *z = reinterpret_cast<const T *>(a.logits) + b * a.ldz + c0;
+  float best;
+  int best_at;
+  const RowSums r = group_joined(walk<T, false, false>(z, cols, a.c, &best, &best_at), a.c, part);
+  if (threadIdx.x == 0) a.sums[blockIdx.x] = r;
+}
+
 struct LogprobsBwdArgs {
-  int V;
+  int V, parts, per;
   const void *logits;
   int64_t ldz;
   const int32_t *tokens;
@@ -88,53 +268,130 @@ struct LogprobsBwdArgs {
   int64_t lddl;
 };
 
+// The gradient: one pass, a workgroup a part of a row.
 template <typename T, typename TO>
-__global__ void __launch_bounds__(256) logprobs_bwd_kernel(LogprobsBwdArgs a) {
-  const int64_t b = blockIdx.x;
-  const T *z = reinterpret_cast<const T *>(a.logits) + b * a.ldz;
-  TO *out = reinterpret_cast<TO *>(a.dlogits) + b * a.lddl;
-  const int t = a.tokens[b];
+__global__ void __launch_bounds__(LP_NT) logprobs_bwd_kernel(LogprobsBwdArgs a) {
+  constexpr int N = chunk_elems<T>();
+  const int tid = threadIdx.x;
+  const int64_t b = blockIdx.x / (unsigned)a.parts;
+  const int p = (int)(blockIdx.x - b * a.parts), c0 = p * a.per, cols = min(a.per, a.V - c0);
+  const T *z = reinterpret_cast<const T *>(a.logits) + b * a.ldz + c0;
+  TO *out = reinterpret_cast<TO *>(a.dlogits) + b * a.lddl + c0;
+  const int t = a.tokens[b], at = t - c0;
   float g = a.dlogp && t >= 0 ? a.dlogp[b] : 0.f;
   const float h = a.dentropy ? a.dentropy[b] : 0.f;
   const bool none = g == 0.f && h == 0.f;
   if (t >= a.V && !none) g = __builtin_nanf("");
   const float lse = a.lse[b], add = h == 0.f ? 0.f : a.entropy[b];
-  for (int64_t v = threadIdx.x; v < a.V; v += 256) {
-    const float lq = __builtin_elementwise_maximum(load_f32(z + v) * a.inv_t - lse, -200.f), q = pow2(lq * LOG2E);
-    const float d = (v == t ? g : 0.f) - q * (g + h * (lq + add));
-    store_f32(out + v, none ? 0.f : d * a.inv_t);
+  g *= a.inv_t;
+  const float hs = h * a.inv_t, base = g + hs * add;
+  auto put = [&](const u32x4 &v, int k, int n) {
+    float d[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float lq = __builtin_elementwise_maximum(chunk_at<T>(v, i) * a.inv_t - lse, -200.f), q = pow2(lq * LOG2E);
+      d[i] = -q * fmaf(hs, lq, base);
+      if (none) d[i] = 0.f;
+    }
+    if (at >= k * N && at < k * N + N && !none) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] += k * N + i == at ? g : 0.f;
+    }
+    store_chunk<TO, N>(out + (int64_t)k * N, d, n);
+  };
+  const int chunks = (cols + N - 1) / N, whole = cols / N;
+  int k = tid;
+  for (; k + (LP_UNROLL - 1) * LP_NT < whole; k += LP_UNROLL * LP_NT) {
+    u32x4 v[LP_UNROLL];
+#pragma unroll
+    for (int q = 0; q < LP_UNROLL; ++q) v[q] = load_chunk(z + (int64_t)(k + q * LP_NT) * N);
+#pragma unroll
+    for (int q = 0; q < LP_UNROLL; ++q) put(v[q], k + q * LP_NT, N);
+  }
+  for (; k < chunks; k += LP_NT) {
+    const T *q = z + (int64_t)k * N;
+    put(k < whole ? load_chunk(q) : load_cut_chunk(q, cols - k * N), k, min(N, cols - k * N));
   }
 }
 
 }  // namespace
 
-size_t logprobs_ws_bytes(int B, int V, int n) { return 0; }
+RowParts row_parts(int B, int V) {
+  int parts = 512 / max(B, 1);
+  parts = min(parts, min(PARTS_MOST, V / 4096));
+  parts = max(parts, 1);
+  const int per = (int)(((int64_t)V + parts - 1) / parts + 7) / 8 * 8;
+  return RowParts{(int)(((int64_t)V + per - 1) / per), per};
+}
+
+size_t logprobs_ws_bytes(int B, int V, int n) {
+  const RowParts cut = row_parts(B, V);
+  return cut.parts == 1 ? 0 : (size_t)B * cut.parts * (sizeof(RowSums) + 8 * (size_t)n);
+}
+
+int run_row_sums(int dtype, int B, int V, const RowParts &cut, const void *logits, int64_t ldz, float c, RowSums *sums,
+                 hipStream_t s) {
+  LogprobsArgs a{};
+  a.V = V; a.parts = cut.parts; a.per = cut.per;
+  a.logits = logits; a.ldz = ldz; a.c = c; a.sums = sums;
+  const dim3 grid((unsigned)B * cut.parts), wg(LP_NT);
+  {
+    LaunchTimer t(IMBD_K_DISTILL, 1, s);
+    if (dtype == IMBD_BF16) hipLaunchKernelGGL(row_sums_kernel<uint16_t>, grid, wg, 0, s, a);
+    else hipLaunchKernelGGL(row_sums_kernel<float>, grid, wg, 0, s, a);
+  }
+  return check_launch("row_sums");
+}
+
+template <typename T>
+static int launch_logprobs(const LogprobsArgs &a, int B, hipStream_t s) {
+  const dim3 grid((unsigned)B * a.parts), wg(LP_NT);
+  {
+    LaunchTimer t(IMBD_K_LOGPROBS, 0, s);
+    if (a.n > 0 && a.entropy) hipLaunchKernelGGL((logprobs_kernel<T, true, true>), grid, wg, 0, s, a);
+    else if (a.n > 0) hipLaunchKernelGGL((logprobs_kernel<T, false, true>), grid, wg, 0, s, a);
+    else if (a.entropy) hipLaunchKernelGGL((logprobs_kernel<T, true, false>), grid, wg, 0, s, a);
+    else hipLaunchKernelGGL((logprobs_kernel<T, false, false>), grid, wg, 0, s, a);
+  }
+  const int rc = check_launch("token_logprobs");
+  if (rc != IMBD_OK || a.parts == 1) return rc;
+  {
+    LaunchTimer t(IMBD_K_LOGPROBS, 1, s);
+    hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3(B), wg, 0, s, a);
+  }
+  return check_launch("token_logprobs (join)");
+}
 
 int run_logprobs(int dtype, int B, int V, int n, const void *logits, int64_t ldz, const int32_t *tokens,
                  float temperature, float *logp, float *entropy, float *lse, int32_t *top_ids, float *top_logp, void *ws,
                  hipStream_t s) {
+  const RowParts cut = row_parts(B, V);
   const float inv_t = 1.0f / temperature;
-  LogprobsArgs a{B, V, n, logits, ldz, tokens, inv_t, inv_t * LOG2E, logp, entropy, lse, top_ids, top_logp};
-  {
-    LaunchTimer t(IMBD_K_LOGPROBS, 0, s);
-    if (dtype == IMBD_BF16) hipLaunchKernelGGL(logprobs_kernel<uint16_t>, dim3(B), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(logprobs_kernel<float>, dim3(B), dim3(256), 0, s, a);
+  LogprobsArgs a{V, n, cut.parts, cut.per, logits, ldz, tokens, inv_t, inv_t * LOG2E, logp, entropy, lse, top_ids, top_logp,
+                 nullptr, nullptr};
+  if (cut.parts > 1) {  // (the keys first: they are 8 bytes)
+    a.keys = reinterpret_cast<uint64_t *>(ws);
+    a.sums = reinterpret_cast<RowSums *>(a.keys + (size_t)B * cut.parts * n);
   }
-  return check_launch("token_logprobs");
+  return dtype == IMBD_BF16 ? launch_logprobs<uint16_t>(a, B, s) : launch_logprobs<float>(a, B, s);
+}
+
+template <typename T>
+static void launch_bwd(const LogprobsBwdArgs &a, int B, int dlogits_dtype, hipStream_t s) {
+  const dim3 grid((unsigned)B * a.parts), wg(LP_NT);
+  if (dlogits_dtype == IMBD_BF16) hipLaunchKernelGGL((logprobs_bwd_kernel<T, uint16_t>), grid, wg, 0, s, a);
+  else hipLaunchKernelGGL((logprobs_bwd_kernel<T, float>), grid, wg, 0, s, a);
 }
 
 int run_logprobs_bwd(int dtype, int B, int V, const void *logits, int64_t ldz, const int32_t *tokens,
                      float temperature, const float *lse, const float *entropy, const float *dlogp,
                      const float *dentropy, void *dlogits, int64_t lddl, int dlogits_dtype, hipStream_t s) {
-  LogprobsBwdArgs a{V, logits, ldz, tokens, 1.0f / temperature, lse, entropy, dlogp, dentropy, dlogits, lddl};
-  const dim3 grid(B), wg(256);
+  const RowParts cut = row_parts(B, V);
+  LogprobsBwdArgs a{V, cut.parts, cut.per, logits, ldz, tokens, 1.0f / temperature, lse, entropy, dlogp, dentropy, dlogits, lddl};
   {
-    LaunchTimer t(IMBD_K_LOGPROBS, 1, s);
-    if (dtype == IMBD_BF16 && dlogits_dtype == IMBD_BF16)
-      hipLaunchKernelGGL((logprobs_bwd_kernel<uint16_t, uint16_t>), grid, wg, 0, s, a);
-    else if (dtype == IMBD_BF16) hipLaunchKernelGGL((logprobs_bwd_kernel<uint16_t, float>), grid, wg, 0, s, a);
-    else if (dlogits_dtype == IMBD_BF16) hipLaunchKernelGGL((logprobs_bwd_kernel<float, uint16_t>), grid, wg, 0, s, a);
-    else hipLaunchKernelGGL((logprobs_bwd_kernel<float, float>), grid, wg, 0, s, a);
+    LaunchTimer t(IMBD_K_LOGPROBS, 2, s);
+    if (dtype == IMBD_BF16) launch_bwd<uint16_t>(a, B, dlogits_dtype, s);
+    else launch_bwd<float>(a, B, dlogits_dtype, s);
   }
   return check_launch("token_logprobs_bwd");
 }

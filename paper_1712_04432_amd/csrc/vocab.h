@@ -8,6 +8,7 @@ namespace imbd {
 
 constexpr int TOP_MOST = 64;         // alternatives
 constexpr int ENTRIES_MOST = 256;    // a teacher's entries of a row
+constexpr int PARTS_MOST = 32;      // of a row
 constexpr int VOCAB_MOST = 1 << 30;
 constexpr int VOCAB_ROWS_MOST = (1 << 24) - 1;  // a workgroup each: 2^32 work-items are a launch's most
 
@@ -34,6 +35,48 @@ template <typename T>
 __device__ __forceinline__ void store_f32(T *p, float v) {
   if constexpr (sizeof(T) == 2) *p = f32_to_bf16(v);
   else *p = v;
+}
+
+// Rows are walked in chunks of 16 bytes, at any element alignment.
+template <typename T>
+constexpr int chunk_elems() { return 16 / (int)sizeof(T); }
+
+template <typename T>
+__device__ __forceinline__ u32x4 load_chunk(const T *p) { return *reinterpret_cast<const u32x4_any *>(p); }
+// ... of which the first n elements exist, the others are -inf
+template <typename T>
+__device__ __forceinline__ u32x4 load_cut_chunk(const T *p, int n) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2)
+      v[i] = (2 * i < n ? p[2 * i] : 0xff80u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0xff800000u);
+    else v[i] = i < n ? __builtin_bit_cast(uint32_t, p[i]) : 0xff800000u;
+  }
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ float chunk_at(const u32x4 &v, int i) {
+  const uint32_t w = v[sizeof(T) == 2 ? i >> 1 : i];  // (a copy: the cast of a vector's element itself takes the first)
+  if constexpr (sizeof(T) == 2) return __builtin_bit_cast(float, i & 1 ? w & 0xffff0000u : w << 16);
+  else return __builtin_bit_cast(float, w);
+}
+// Stores the chunk's N values (N: of the logits' chunk), n of them real.
+template <typename TO, int N>
+__device__ __forceinline__ void store_chunk(TO *p, const float (&v)[N], int n) {
+  if (n < N) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) store_f32(p + i, v[i]);
+  } else if constexpr (sizeof(TO) == 4) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4_any *>(p + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+  } else if constexpr (N == 8) {
+    *reinterpret_cast<u32x4_any *>(p) = u32x4{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]),
+                                              cvt_pk_bf16(v[6], v[7])};
+  } else {
+    *reinterpret_cast<u32x2_any *>(p) = u32x2{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
+  }
 }
 
 // What a softmax over a row needs, over part of it: m a reference (near the largest logit), s the sum of
@@ -67,6 +110,23 @@ __device__ __forceinline__ RowSums wave_joined(RowSums r, float c) {
     const RowSums b{__shfl_xor(r.m, o, 64), __shfl_xor(r.s, o, 64), __shfl_xor(r.u, o, 64)};
     r = joined(r, b, c);
   }
+  return r;
+}
+
+
+// Long rows are cut into parts, a workgroup each, where the rows are too few to fill the GPU: `parts` of `per` columns (a
+// multiple of 8; the last shorter).
+struct RowParts {
+  int parts, per;
+};
+RowParts row_parts(int B, int V);
+// The sums of every part of every row, [b][part] (one part: of every row). Only the sums m and s.
+int run_row_sums(int dtype, int B, int V, const RowParts &cut, const void *logits, int64_t ldz, float c, RowSums *sums,
+                 hipStream_t s);
+// All parts of a row, joined in their order.
+__device__ __forceinline__ RowSums joined_parts(const RowSums *sums, int parts, float c) {
+  RowSums r = sums[0];
+  for (int i = 1; i < parts; ++i) r = joined(r, sums[i], c);
   return r;
 }
 
