@@ -22,17 +22,6 @@ struct DistillArgs {
   int64_t lddl;
 };
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-__device__ __forceinline__ float wave_max(float v) {  // (a NaN stays one)
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v = __builtin_elementwise_maximum(v, __shfl_xor(v, o, 64));
-  return v;
-}
-
 template <typename T, typename TO>
 __global__ void __launch_bounds__(256) distill_kernel(DistillArgs a) {
   __shared__ RowSums part[4];
@@ -44,7 +33,7 @@ __global__ void __launch_bounds__(256) distill_kernel(DistillArgs a) {
   const T *z = reinterpret_cast<const T *>(a.logits) + b * a.ldz;
   TO *out = a.dlogits ? reinterpret_cast<TO *>(a.dlogits) + b * a.lddl : nullptr;
   auto all_max = [&](float v) {
-    v = wave_max(v);
+    v = wave_maximum(v);
     __syncthreads();
     if (lane == 0) red[wave] = v;
     __syncthreads();

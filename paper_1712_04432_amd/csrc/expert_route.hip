@@ -20,6 +20,7 @@
 // 4.6 and 4.4); 16 tokens, k = 4, 5.0 us in one launch (least 4.8).
 
 #include "expert.h"
+#include "lanes.h"
 #include "order_key.h"
 
 namespace imbd {
@@ -28,16 +29,6 @@ namespace {
 constexpr int RT_NT = 1024;      // threads of a workgroup
 constexpr int RT_BLOCKS = 256;   // workgroups at most (rows of the table)
 
-// The value of the lane that a group's reduction pairs with at distance o: inside 16 lanes by the cross-lane forms
-// of the vector instructions (at 4 and 8 the mirrored lane, which holds the same as its neighbours by then).
-template <int o>
-__device__ __forceinline__ int partner(int v) {
-  if constexpr (o == 1) return __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, false);        // quad: 1 0 3 2
-  else if constexpr (o == 2) return __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, false);   // quad: 2 3 0 1
-  else if constexpr (o == 4) return __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, false);  // half rows mirrored
-  else if constexpr (o == 8) return __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, false);  // rows mirrored
-  else return __shfl_xor(v, o, 64);
-}
 template <int G, int o = 1>
 __device__ __forceinline__ uint32_t group_max(uint32_t v) {
   if constexpr (o >= G) return v;

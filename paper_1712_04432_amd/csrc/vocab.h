@@ -3,6 +3,7 @@
 #pragma once
 
 #include "cdna4.h"
+#include "lanes.h"
 
 namespace imbd {
 
@@ -104,15 +105,11 @@ __device__ __forceinline__ RowSums joined(const RowSums &a, const RowSums &b, fl
   const RowSums x = moved(a, m, c), y = moved(b, m, c);
   return RowSums{m, x.s + y.s, x.u + y.u};
 }
-__device__ __forceinline__ RowSums wave_joined(RowSums r, float c) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const RowSums b{__shfl_xor(r.m, o, 64), __shfl_xor(r.s, o, 64), __shfl_xor(r.u, o, 64)};
-    r = joined(r, b, c);
-  }
-  return r;
+// All lanes' sums, in each of them.
+__device__ __forceinline__ RowSums wave_joined(const RowSums &r, float c) {
+  const RowSums x = moved(r, wave_max(r.m), c);
+  return RowSums{x.m, wave_sum(x.s), wave_sum(x.u)};
 }
-
 
 // Long rows are cut into parts, a workgroup each, where the rows are too few to fill the GPU: `parts` of `per` columns (a
 // multiple of 8; the last shorter).
@@ -123,11 +120,10 @@ RowParts row_parts(int B, int V);
 // The sums of every part of every row, [b][part] (one part: of every row). Only the sums m and s.
 int run_row_sums(int dtype, int B, int V, const RowParts &cut, const void *logits, int64_t ldz, float c, RowSums *sums,
                  hipStream_t s);
-// All parts of a row, joined in their order.
+// All parts of a row, joined by every wave for itself (PARTS_MOST <= 64).
 __device__ __forceinline__ RowSums joined_parts(const RowSums *sums, int parts, float c) {
-  RowSums r = sums[0];
-  for (int i = 1; i < parts; ++i) r = joined(r, sums[i], c);
-  return r;
+  const int lane = threadIdx.x & 63;
+  return wave_joined(lane < parts ? sums[lane] : RowSums{LOWEST, 0.f, 0.f}, c);
 }
 
 }  // namespace imbd
