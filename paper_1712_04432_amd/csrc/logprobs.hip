@@ -15,13 +15,13 @@
 // and gradient of 8192 rows of 32768 311 us (5.2 TB/s).
 
 #include "order_key.h"
+#include "row_walk.h"
 #include "vocab.h"
 
 namespace imbd {
 namespace {
 
-constexpr int LP_NT = 256;     // threads of a workgroup
-constexpr int LP_UNROLL = 4;   // chunks of a thread in flight
+constexpr int LP_NT = WALK_NT, LP_UNROLL = WALK_UNROLL;
 constexpr int LP_LIST = 1024;  // candidates
 
 struct LogprobsArgs {
@@ -82,67 +82,6 @@ __device__ __forceinline__ void put_row(const LogprobsArgs &a, int64_t b, const 
 __device__ __forceinline__ void put_choice(const LogprobsArgs &a, int64_t b, int j, uint64_t key, const RowSums &r, float ls) {
   a.top_ids[b * a.n + j] = key ? (int)~(uint32_t)key : -1;
   a.top_logp[b * a.n + j] = key ? (key_value((uint32_t)(key >> 32)) - r.m) * a.inv_t - ls : -INFINITY;
-}
-
-// One workgroup's part of a row. ENT: with u. TOP: remembers where the thread's largest logit is.
-template <typename T, bool ENT, bool TOP>
-__device__ __forceinline__ RowSums walk(const T *z, int cols, float c, float *best, int *best_at) {
-  constexpr int N = chunk_elems<T>();
-  const int tid = threadIdx.x, chunks = (cols + N - 1) / N, whole = cols / N;
-  const float slack = 16.f / c;
-  RowSums r{LOWEST, 0.f, 0.f};
-  auto take = [&](const auto &v, int first) {
-    constexpr int M = sizeof(v) / 16;
-    float top = -INFINITY;
-#pragma unroll
-    for (int q = 0; q < M; ++q) {
-      float cm = chunk_at<T>(v[q], 0);
-#pragma unroll
-      for (int i = 1; i < N; ++i) cm = fmaxf(cm, chunk_at<T>(v[q], i));
-      if constexpr (TOP) {
-        const bool more = cm > *best;
-        *best = more ? cm : *best;
-        *best_at = more ? first + q * LP_NT : *best_at;
-      }
-      top = fmaxf(top, cm);
-    }
-    if (top > r.m + slack) r = moved(r, top, c);
-#pragma unroll
-    for (int q = 0; q < M; ++q) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float x = chunk_at<T>(v[q], i);
-        if constexpr (ENT) {
-          const float d = scaled(x, r.m, c), e = pow2(d);
-          r.s += e;
-          r.u = fmaf(e, d, r.u);
-        } else {
-          r.s += pow2((x - r.m) * c);
-        }
-      }
-    }
-  };
-  int k = tid;
-  for (; k + (LP_UNROLL - 1) * LP_NT < whole; k += LP_UNROLL * LP_NT) {
-    u32x4 v[LP_UNROLL];
-#pragma unroll
-    for (int q = 0; q < LP_UNROLL; ++q) v[q] = load_chunk(z + (int64_t)(k + q * LP_NT) * N);
-    take(v, k);
-  }
-  for (; k < chunks; k += LP_NT) {
-    u32x4 v[1];
-    v[0] = k < whole ? load_chunk(z + (int64_t)k * N) : load_cut_chunk(z + (int64_t)k * N, cols - k * N);
-    take(v, k);
-  }
-  return r;
-}
-
-__device__ __forceinline__ RowSums group_joined(RowSums r, float c, RowSums *part) {
-  const int tid = threadIdx.x;
-  r = wave_joined(r, c);
-  if ((tid & 63) == 0) part[tid >> 6] = r;
-  __syncthreads();
-  return joined(joined(part[0], part[1], c), joined(part[2], part[3], c), c);
 }
 
 template <typename T, bool ENT, bool TOP>
@@ -268,18 +207,6 @@ __global__ void __launch_bounds__(LP_NT) logprobs_join_kernel(LogprobsArgs a) {
   put_in_order(keys, found, a.n, [&](int j, uint64_t key) { put_choice(a, b, j, key, r, ls); });
 }
 
-template <typename T>
-__global__ void __launch_bounds__(LP_NT) row_sums_kernel(LogprobsArgs a) {
-  __shared__ RowSums part[LP_NT / 64];
-  const int64_t b = blockIdx.x / (unsigned)a.parts;
-  const int p = (int)(blockIdx.x - b * a.parts), c0 = p * a.per, cols = min(a.per, a.V - c0);
-  const T *z = reinterpret_cast<const T *>(a.logits) + b * a.ldz + c0;
-  float best;
-  int best_at;
-  const RowSums r = group_joined(walk<T, false, false>(z, cols, a.c, &best, &best_at), a.c, part);
-  if (threadIdx.x == 0) a.sums[blockIdx.x] = r;
-}
-
 struct LogprobsBwdArgs {
   int V, parts, per;
   const void *logits;
@@ -353,20 +280,6 @@ RowParts row_parts(int B, int V) {
 size_t logprobs_ws_bytes(int B, int V, int n) {
   const RowParts cut = row_parts(B, V);
   return cut.parts == 1 ? 0 : (size_t)B * cut.parts * (sizeof(RowSums) + 8 * (size_t)n);
-}
-
-int run_row_sums(int dtype, int B, int V, const RowParts &cut, const void *logits, int64_t ldz, float c, RowSums *sums,
-                 hipStream_t s) {
-  LogprobsArgs a{};
-  a.V = V; a.parts = cut.parts; a.per = cut.per;
-  a.logits = logits; a.ldz = ldz; a.c = c; a.sums = sums;
-  const dim3 grid((unsigned)B * cut.parts), wg(LP_NT);
-  {
-    LaunchTimer t(IMBD_K_DISTILL, 1, s);
-    if (dtype == IMBD_BF16) hipLaunchKernelGGL(row_sums_kernel<uint16_t>, grid, wg, 0, s, a);
-    else hipLaunchKernelGGL(row_sums_kernel<float>, grid, wg, 0, s, a);
-  }
-  return check_launch("row_sums");
 }
 
 template <typename T>

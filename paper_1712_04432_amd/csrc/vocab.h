@@ -117,9 +117,6 @@ struct RowParts {
   int parts, per;
 };
 RowParts row_parts(int B, int V);
-// The sums of every part of every row, [b][part] (one part: of every row). Only the sums m and s.
-int run_row_sums(int dtype, int B, int V, const RowParts &cut, const void *logits, int64_t ldz, float c, RowSums *sums,
-                 hipStream_t s);
 // All parts of a row, joined by every wave for itself (PARTS_MOST <= 64).
 __device__ __forceinline__ RowSums joined_parts(const RowSums *sums, int parts, float c) {
   const int lane = threadIdx.x & 63;
