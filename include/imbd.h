@@ -207,6 +207,54 @@ int mlp_local_bwd(int dtype, int P_r, int P_c, int d_out_blk, int d_in, int b_bl
 size_t mlp_local_workspace_bytes(int which, int dtype, int d_out_blk, int d_in, int b_blk);
 
 /* ====================================================================================
+ * A fully connected layer of any network: the product of Sec. 1 with an activation of choice and
+ * a residual in its epilogue, and the products of its backward pass with the derivative of
+ * the activation below and the residual's gradient in theirs. Layouts as for the local blocks: w
+ * [d_out][ldw], x [B][ldx] in dtype, one sample per row; any strides, any alignment.
+ * Sizes (IMBD_EUNSUPPORTED past them): widths up to 2^30, fewer than 2^31 - 1024 samples, and no launch of 2^24
+ * workgroups or more. No output may overlap an input or another output, but for a residual in the
+ * place of the output that it is added to (same address, leading dimension and type).
+ * ==================================================================================== */
+enum imbd_act {
+    IMBD_ACT_NONE = 0,      /* v */
+    IMBD_ACT_RELU = 1,      /* max(v, 0); derivative 1 where v > 0 */
+    IMBD_ACT_GELU = 2,      /* v Phi(v), Phi the standard normal distribution */
+    IMBD_ACT_GELU_TANH = 3, /* v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2 */
+    IMBD_ACT_SILU = 4       /* v / (1 + e^-v) */
+};
+
+/* Workspace bytes for linear_fwd (which = 0) or linear_bwd (which = 1) at these sizes: 0 for
+ * sizes that they refuse, and maybe for others (then ws is not read). ws is 256-byte aligned. */
+size_t linear_workspace_bytes(int which, int dtype, int d_out, int d_in, int B);
+
+/* z = W x + bias,  y = act(z) + residual. bias [d_out] fp32 or NULL; residual [B][ldr] in y_dtype or
+ * NULL; y [B][ldy] in y_dtype; z [B][ldz] in dtype, or NULL: not kept (linear_bwd of the layer above
+ * needs it unless act is none). Sums, act and residual in fp32, y and z rounded once each (y
+ * does not see z's rounding). */
+int linear_fwd(int dtype, int act, int d_out, int d_in, int B, const void *w, int64_t ldw,
+               const float *bias, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+               void *y, int64_t ldy, int y_dtype, void *z, int64_t ldz, void *ws, size_t ws_bytes,
+               void *stream);
+
+/* The backward products, each skipped where its output is NULL (not all three). dy [B][lddy] in
+ * dtype is the gradient before this layer's own activation, at W x + bias:
+ *   dx = (W^T dy) * act'(z) + residual     x = act(z) is the output of the layer below
+ *   dw[o][i] = sum_b dy[b][o] x[b][i]      db[o] = sum_b dy[b][o]
+ * so that dx is the dy of the layer below (or, with act none, the gradient of x itself). z [B][ldz]
+ * in dtype, not read where act is none; residual [B][ldr] in dx_dtype or NULL: what else flows back
+ * to the same place; dx [B][lddx] in dx_dtype; dw [d_out][lddw] and db [d_out] fp32. w may be NULL
+ * without dx, x without dw. B == 0 writes zeros to dw and db. */
+int linear_bwd(int dtype, int act, int d_out, int d_in, int B, const void *w, int64_t ldw,
+               const void *dy, int64_t lddy, const void *x, int64_t ldx, float *dw, int64_t lddw,
+               float *db, const void *z, int64_t ldz, const void *residual, int64_t ldr, void *dx,
+               int64_t lddx, int dx_dtype, void *ws, size_t ws_bytes, void *stream);
+
+/* dz = dy * act'(z), d columns, all in dtype: for a layer whose own activation is followed by a residual, dy the
+ * gradient of its y. (A residual itself receives dy.) dz may be dy or z (same leading dimension). */
+int act_bwd(int dtype, int act, int B, int d, const void *dy, int64_t lddy, const void *z, int64_t ldz,
+            void *dz, int64_t lddz, void *stream);
+
+/* ====================================================================================
  * Domain-parallel 3x3 convolution tile (Sec. 2.2, Fig. of the domain split; sizes from
  * Eq. (2)). Stride 1, "same" padding, cross-correlation, channels-last bf16 operands:
  *   x_pad  [N][H+2][W+2][C_in]  : the tile plus its 1-pixel halo (zeros on the image border)

@@ -22,7 +22,8 @@ from ._abi import (IMBD_BF16, IMBD_F32, IMBD_K_BIAS, IMBD_K_CAST, IMBD_K_CONV_DG
                    IMBD_EINVAL, IMBD_EUNSUPPORTED, IMBD_EHIP, IMBD_EWORKSPACE,
                    IMBD_WS_ACT, IMBD_WS_DY, IMBD_WS_LOGITS, IMBD_WS_ROWLOSS, AdamWTensor, ImbdError,
                    Layer, MlpDesc, check, load)
-from ._abi import IMBD_STATIC_SCRATCH_BYTES  # noqa: F401
+from ._abi import (IMBD_ACT_GELU, IMBD_ACT_GELU_TANH, IMBD_ACT_NONE, IMBD_ACT_RELU, IMBD_ACT_SILU,  # noqa: F401
+                   IMBD_STATIC_SCRATCH_BYTES)
 from ._abi import (IMBD_OPT_CONV_NT, IMBD_OPT_COUNT, IMBD_OPT_DW_GENERIC, IMBD_OPT_DW_STREAM,  # noqa: F401
                    IMBD_OPT_DW_WIDE_DUAL, IMBD_OPT_DW_WIDE_MIN_K, IMBD_OPT_LOCAL_PAIR, IMBD_OPT_GEMM_CFG, IMBD_OPT_GEMM_SPLITS, IMBD_OPT_SKINNY_OFF,
                    IMBD_OPT_SKINNY_NB, IMBD_OPT_SKINNY_SPLITS, IMBD_OPT_TOP_UNFUSED, IMBD_OPT_WIDE_OFF,
@@ -36,7 +37,7 @@ __all__ = [
     "timing_end",
     "expert_route_workspace_bytes", "expert_route", "expert_route_bwd", "expert_fwd", "expert_bwd",
     "expert_combine", "expert_combine_bwd", "AdamW", "adamw_step",
-    "distill_workspace_bytes", "distill_xent", "token_logprobs_workspace_bytes", "token_logprobs", "token_logprobs_bwd",
+    "linear_workspace_bytes", "linear_fwd", "linear_bwd", "act_bwd", "distill_workspace_bytes", "distill_xent", "token_logprobs_workspace_bytes", "token_logprobs", "token_logprobs_bwd",
     "ws_view", "dtype_code", "set_option", "get_option", "option_name", "options",
 ]
 
@@ -429,6 +430,74 @@ def expert_combine_bwd(dy, ys, slots, gates, dys, dgates=None, stream=None):
                                  _sizes(gates, (T, k), f32, "gates", dev, True), _sizes(dys, (n, d), dt, "dys", dev),
                                  _rows_ld(dys), None if dgates is None else _sizes(dgates, (T, k), f32, "dgates", dev, True),
                                  _on(stream, dev)), "expert_combine_bwd")
+
+
+# --------------------------------- a fully connected layer with activation and residual
+# (Checked as the expert layer's tensors are.)
+_ACTS = {"none": IMBD_ACT_NONE, "relu": IMBD_ACT_RELU, "gelu": IMBD_ACT_GELU, "gelu_tanh": IMBD_ACT_GELU_TANH,
+         "silu": IMBD_ACT_SILU}
+
+
+def _act(act):
+    if act not in _ACTS:
+        raise ValueError(f"act {act!r}: one of {', '.join(_ACTS)}")
+    return _ACTS[act]
+
+
+def _matrix(t, shape, dtype, name, device):
+    """Address and leading dimension of an optional matrix."""
+    return (None, 0) if t is None else (_sizes(t, shape, dtype, name, device), _rows_ld(t))
+
+
+def linear_workspace_bytes(which: int, dtype_: int, d_out: int, d_in: int, B: int) -> int:
+    if max(d_out, d_in, B) >> 31 > 0:
+        _too_large(d_out, d_in, B)
+    return load().linear_workspace_bytes(which, dtype_, d_out, d_in, B)
+
+
+def linear_fwd(w, x, y, bias=None, act: str = "none", residual=None, z=None, ws=None, stream=None):
+    """y = act(W x + bias) + residual; z keeps W x + bias. act: none, relu, gelu, gelu_tanh or silu."""
+    lib, dev = load(), _here(w, "w")
+    d_out, d_in = w.shape
+    B = x.shape[0]
+    if (d_out | d_in | B) >> 31:
+        _too_large(d_out, d_in, B)
+    (dt, code), (ydt, ycode) = _float(w, "w"), _float(y, "y")
+    at_ws, ws_bytes = _ws(ws, dev)
+    check(lib.linear_fwd(code, _act(act), d_out, d_in, B, *_matrix(w, (d_out, d_in), dt, "w", dev),
+                         _opt(bias, (d_out,), _torch().float32, "bias", dev), *_matrix(x, (B, d_in), dt, "x", dev),
+                         *_matrix(residual, (B, d_out), ydt, "residual", dev), *_matrix(y, (B, d_out), ydt, "y", dev),
+                         ycode, *_matrix(z, (B, d_out), dt, "z", dev), at_ws, ws_bytes, _on(stream, dev)), "linear_fwd")
+
+
+def linear_bwd(w, dy, x, dw=None, db=None, dx=None, act: str = "none", z=None, residual=None, ws=None, stream=None):
+    """The backward products of linear_fwd, dy the gradient of W x + bias: dw, db, and dx = (W^T dy) * act'(z) + residual
+    with the activation and the z of the layer below. What is None is skipped; w gives the sizes also where dx is
+    None, x may be None without dw."""
+    lib, dev, f32 = load(), _here(w, "w"), _torch().float32
+    d_out, d_in = w.shape
+    B = dy.shape[0]
+    if (d_out | d_in | B) >> 31:
+        _too_large(d_out, d_in, B)
+    dt, code = _float(w, "w")
+    dxdt, dxcode = (dt, code) if dx is None else _float(dx, "dx")
+    at_ws, ws_bytes = _ws(ws, dev)
+    check(lib.linear_bwd(code, _act(act), d_out, d_in, B, *_matrix(w, (d_out, d_in), dt, "w", dev),
+                         *_matrix(dy, (B, d_out), dt, "dy", dev), *_matrix(x, (B, d_in), dt, "x", dev),
+                         *_matrix(dw, (d_out, d_in), f32, "dw", dev), _opt(db, (d_out,), f32, "db", dev),
+                         *_matrix(z, (B, d_in), dt, "z", dev), *_matrix(residual, (B, d_in), dxdt, "residual", dev),
+                         *_matrix(dx, (B, d_in), dxdt, "dx", dev), dxcode, at_ws, ws_bytes, _on(stream, dev)), "linear_bwd")
+
+
+def act_bwd(dy, z, dz, act: str, stream=None):
+    """dz = dy * act'(z) (dz may be dy or z)."""
+    lib, dev = load(), _here(dy, "dy")
+    B, d = dy.shape
+    if (B | d) >> 31:
+        _too_large(B, d)
+    dt, code = _float(dy, "dy")
+    check(lib.act_bwd(code, _act(act), B, d, *_matrix(dy, (B, d), dt, "dy", dev), *_matrix(z, (B, d), dt, "z", dev),
+                      *_matrix(dz, (B, d), dt, "dz", dev), _on(stream, dev)), "act_bwd")
 
 
 # ------------------------------------------------- what a vocabulary's logits are for

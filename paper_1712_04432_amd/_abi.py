@@ -16,6 +16,7 @@ IMBD_WS_ACT, IMBD_WS_LOGITS, IMBD_WS_DY, IMBD_WS_ROWLOSS = 0, 1, 2, 3
  IMBD_OPT_REDUCE_TAIL) = range(15)
 IMBD_OPT_COUNT = 15
 IMBD_STATIC_SCRATCH_BYTES = 64 << 20
+IMBD_ACT_NONE, IMBD_ACT_RELU, IMBD_ACT_GELU, IMBD_ACT_GELU_TANH, IMBD_ACT_SILU = range(5)
 (IMBD_K_GEMM_FWD, IMBD_K_GEMM_DX, IMBD_K_GEMM_DW, IMBD_K_SPLITK, IMBD_K_SOFTMAX, IMBD_K_BIAS,
  IMBD_K_SGD, IMBD_K_CAST, IMBD_K_CONV_FWD, IMBD_K_CONV_DGRAD, IMBD_K_CONV_WGRAD, IMBD_K_EXPERT_FWD,
  IMBD_K_EXPERT_DX, IMBD_K_EXPERT_DW, IMBD_K_ROUTE, IMBD_K_COMBINE, IMBD_K_ADAMW, IMBD_K_DISTILL, IMBD_K_LOGPROBS,
@@ -73,6 +74,10 @@ SIGNATURES = {
                         _p]),
     "expert_combine": (_i, [_i, _i, _i, _i, _i, _p, _l, _p, _p, _p, _l, _i, _p]),
     "expert_combine_bwd": (_i, [_i, _i, _i, _i, _i, _p, _l, _p, _l, _p, _p, _p, _l, _p, _p]),
+    "linear_workspace_bytes": (_z, [_i, _i, _i, _i, _i]),
+    "linear_fwd": (_i, [_i, _i, _i, _i, _i, _p, _l, _p, _p, _l, _p, _l, _p, _l, _i, _p, _l, _p, _z, _p]),
+    "linear_bwd": (_i, [_i, _i, _i, _i, _i, _p, _l, _p, _l, _p, _l, _p, _l, _p, _p, _l, _p, _l, _p, _l, _i, _p, _z, _p]),
+    "act_bwd": (_i, [_i, _i, _i, _i, _p, _l, _p, _l, _p, _l, _p]),
     "distill_workspace_bytes": (_z, [_i, _i, _i]),
     "distill_xent": (_i, [_i, _i, _i, _i, _p, _l, _p, _p, _p, _p, _f, _f, _p, _p, _p, _l, _i, _p, _z, _p]),
     "token_logprobs_workspace_bytes": (_z, [_i, _i, _i]),

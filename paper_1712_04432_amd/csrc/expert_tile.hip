@@ -23,7 +23,7 @@
 
 #include <type_traits>
 
-#include "expert.h"
+#include "dense.h"
 
 namespace imbd {
 namespace {
@@ -163,8 +163,10 @@ __device__ __forceinline__ bool positive(T v) {
 
 // TM, TN: columns (m) and rows (n) of a tile. GATHER: Delta_W with x's rows by index. (An instance for each way: with both
 // in one, fp32 Delta_W took 141 registers instead of 117 and 127, and three waves a SIMD instead of four.)
-template <typename T, int PASS, int TM, int TN, bool GATHER>
-__global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int tiles_m, int tiles_n) {
+// A: ExpertArgs, or DenseArgs for one layer without experts (K in ranges, its own epilogue).
+template <typename T, int PASS, int TM, int TN, bool GATHER, typename A>
+__global__ void __launch_bounds__(256, 2) expert_tile_kernel(A a, int tiles_m, int tiles_n) {
+  constexpr bool DENSE = std::is_same<A, DenseArgs>::value;
   constexpr int VEC = 16 / (int)sizeof(T);
   constexpr int BK = 8 * VEC;
   constexpr int STAGE = (TM + TN) * XT_PITCH;
@@ -185,7 +187,20 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
     if (e >= a.E) return;
     n0 = (t - e * tiles_n) * TN;
     n_end = a.d_out;
-    expert_range(a, e, &r0, &K);
+    if constexpr (DENSE) {
+      e = __builtin_amdgcn_readfirstlane(e);
+      r0 = e * a.chunk;
+      K = __builtin_amdgcn_readfirstlane(min(a.chunk, a.n_rows - r0));
+    } else {
+      expert_range(a, e, &r0, &K);
+    }
+  } else if constexpr (DENSE) {
+    const int t = bid / tiles_m;
+    e = __builtin_amdgcn_readfirstlane(t / tiles_n);
+    if (e >= a.E) return;
+    n0 = __builtin_amdgcn_readfirstlane((t - e * tiles_n) * TN);
+    n_end = a.n_rows;
+    K = __builtin_amdgcn_readfirstlane(min(a.chunk, (PASS == EXPERT_FWD ? a.d_in : a.d_out) - e * a.chunk));
   } else {
     if (!find_row_tile<TN>(a, bid / tiles_m, &e, &n0, &n_end)) return;
     K = PASS == EXPERT_FWD ? a.d_in : a.d_out;
@@ -194,6 +209,12 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
   const T *w = reinterpret_cast<const T *>(a.w) + (int64_t)e * a.sw;
   const T *x = reinterpret_cast<const T *>(a.x);
   const T *dy = reinterpret_cast<const T *>(a.dy);
+  if constexpr (DENSE && PASS != EXPERT_DW) {  // the range's k
+    const int64_t k0 = (int64_t)e * a.chunk;
+    w += PASS == EXPERT_FWD ? k0 : k0 * a.ldw;
+    if constexpr (PASS == EXPERT_FWD) x += k0;
+    else dy += k0;
+  }
   auto x_row = [&](int s) -> const T * {
     const int r = a.rows ? a.rows[s] : s;
     return r >= 0 && r < a.n_x ? x + (int64_t)r * a.ldx : nullptr;
@@ -387,14 +408,22 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
     const int nl = RPP * p + tid / TPR, n = n0 + nl;
     if (n >= n_end) continue;
     f32x4 v = *reinterpret_cast<const f32x4 *>(stg + nl * PT + (tid % TPR) * 4);
-    if constexpr (PASS == EXPERT_FWD) {
+    if constexpr (DENSE && PASS != EXPERT_DW) {
+      if (a.E == 1) {
+        float q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = v[i] + bias[i];
+        dense_finish<T, PASS>(a, n, m, cnt, q);
+        continue;
+      }
+    } else if constexpr (PASS == EXPERT_FWD) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         v[q] += bias[q];
         if (a.relu) v[q] = v[q] < 0.f ? 0.f : v[q];  // (a NaN stays one)
       }
     }
-    if constexpr (PASS == EXPERT_DX) {
+    if constexpr (PASS == EXPERT_DX && !DENSE) {
       if (a.mask) {
         const T *mk = x_row(n);
 #pragma unroll
@@ -402,8 +431,8 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(ExpertArgs a, int t
           if (!(mk && q < cnt && positive<T>(mk[m + q]))) v[q] = 0.f;
       }
     }
-    const int64_t at = (PASS == EXPERT_DW ? (int64_t)e * a.so : 0) + (int64_t)n * a.ldo + m;
-    if (a.out_dtype == IMBD_BF16) {
+    const int64_t at = (PASS == EXPERT_DW || DENSE ? (int64_t)e * a.so : 0) + (int64_t)n * a.ldo + m;
+    if (!DENSE && a.out_dtype == IMBD_BF16) {
       uint16_t *o = reinterpret_cast<uint16_t *>(a.out) + at;
       if (cnt == 4) *reinterpret_cast<u32x2_any *>(o) = u32x2{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
       else
@@ -439,9 +468,9 @@ static int launch(const ExpertArgs &a, bool check, hipStream_t s) {
   {
     LaunchTimer t(IMBD_K_EXPERT_FWD + PASS, 0, s);
     if (PASS == EXPERT_DW && a.rows)
-      hipLaunchKernelGGL((expert_tile_kernel<T, PASS, TM, TN, PASS == EXPERT_DW>), grid, wg, 0, s, a, cm, cn);
+      hipLaunchKernelGGL((expert_tile_kernel<T, PASS, TM, TN, PASS == EXPERT_DW, ExpertArgs>), grid, wg, 0, s, a, cm, cn);
     else
-      hipLaunchKernelGGL((expert_tile_kernel<T, PASS, TM, TN, false>), grid, wg, 0, s, a, cm, cn);
+      hipLaunchKernelGGL((expert_tile_kernel<T, PASS, TM, TN, false, ExpertArgs>), grid, wg, 0, s, a, cm, cn);
   }
   return check_launch("expert_tile");
 }
@@ -472,6 +501,45 @@ static int launch_pass(int pass, const ExpertArgs &a, bool check, hipStream_t s)
 
 int run_expert_tile(int pass, int dtype, const ExpertArgs &a, bool check, hipStream_t s) {
   return dtype == IMBD_BF16 ? launch_pass<uint16_t>(pass, a, check, s) : launch_pass<float>(pass, a, check, s);
+}
+
+// ------------------------------------------------------------- one layer without experts
+template <typename T, int PASS, int TM, int TN>
+static int launch_dense(const DenseArgs &a, bool check, hipStream_t s) {
+  const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in, N = PASS == EXPERT_DW ? a.d_out : a.n_rows;
+  const int64_t tm = PASS == EXPERT_DW && !a.out ? 1 : (M + TM - 1) / TM, tn = ((int64_t)N + TN - 1) / TN, blocks = a.E * tn * tm;
+  if (blocks > WORKGROUPS_MOST - 255) {
+    set_error("layer product: %lld tiles are more than one launch takes", (long long)blocks);
+    return IMBD_EUNSUPPORTED;
+  }
+  if (blocks == 0 || check) return IMBD_OK;
+  const dim3 grid((unsigned)((blocks + 255) / 256 * 256));
+  {
+    LaunchTimer t(IMBD_K_LINEAR, PASS, s);
+    hipLaunchKernelGGL((expert_tile_kernel<T, PASS, TM, TN, false, DenseArgs>), grid, dim3(256), 0, s, a, (int)tm, (int)tn);
+  }
+  return check_launch("linear_tile");
+}
+
+// The larger tile by the same rule as the expert layer's, over all ranges of K.
+template <typename T, int PASS>
+static int launch_dense_sized(const DenseArgs &a, bool check, hipStream_t s) {
+  constexpr int SIDE = sizeof(T) == 2 || PASS == EXPERT_DX ? 128 : 64;
+  const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in, N = PASS == EXPERT_DW ? a.d_out : a.n_rows;
+  const int64_t squares = (int64_t)a.E * ((M + SIDE - 1) / SIDE) * (((int64_t)N + SIDE - 1) / SIDE);
+  return squares >= (SIDE == 128 ? 256 : 1024) ? launch_dense<T, PASS, SIDE, 64>(a, check, s)
+                                              : launch_dense<T, PASS, 64, 32>(a, check, s);
+}
+
+template <typename T>
+static int launch_dense_pass(int pass, const DenseArgs &a, bool check, hipStream_t s) {
+  return pass == EXPERT_FWD  ? launch_dense_sized<T, EXPERT_FWD>(a, check, s)
+         : pass == EXPERT_DX ? launch_dense_sized<T, EXPERT_DX>(a, check, s)
+                             : launch_dense_sized<T, EXPERT_DW>(a, check, s);
+}
+
+int run_dense_tile(int pass, int dtype, const DenseArgs &a, bool check, hipStream_t s) {
+  return dtype == IMBD_BF16 ? launch_dense_pass<uint16_t>(pass, a, check, s) : launch_dense_pass<float>(pass, a, check, s);
 }
 
 }  // namespace imbd
