@@ -117,7 +117,17 @@ __device__ __forceinline__ void dense_finish(const DenseArgs &a, int n, int m, i
 }
 
 // The products' launches (one range of K or several). check: as for the expert layer's.
+// Any sizes, strides and alignments (csrc/expert_tile.hip).
 int run_dense_tile(int pass, int dtype, const DenseArgs &a, bool check, hipStream_t s);
+// bf16, rows of whole 16-byte chunks (csrc/linear_wide.hip): whether it takes the call, the plan of M x N outputs (rows
+// of a tile, ranges of K and their length, cycles), and the launch.
+struct DensePlan {
+  int bn, ranges, chunk;
+  double cost;
+};
+bool dense_wide_fits(int pass, int dtype, const DenseArgs &a);
+DensePlan dense_wide_plan(int pass, int64_t M, int64_t N, int64_t K);
+int run_dense_wide(int pass, const DenseArgs &a, int bn, bool check, hipStream_t s);
 
 // C entry points' launches (csrc/linear.hip).
 struct LinearArgs {

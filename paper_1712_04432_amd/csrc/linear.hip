@@ -90,13 +90,32 @@ size_t range_bytes(const Ranges &r, int64_t M, int64_t N, bool db) {
   return r.n <= 1 ? 0 : (size_t)r.n * (size_t)(N * partial_ld8((int)M) + (db ? N : 0)) * 4;
 }
 
+// Whether the large tiles take a product that they can take: not while its rows are few (or, for Delta_W, its outputs).
+bool wide_pays(int pass, int64_t M, int64_t N, int64_t K) { return pass == EXPERT_DW ? M >= 64 && N >= 64 : N > 64; }
+
+size_t product_bytes(int pass, int dtype, int64_t M, int64_t N, int64_t K) {
+  const bool db = pass == EXPERT_DW;
+  size_t n = range_bytes(tile_ranges(dtype, M, N, K), M, N, db);
+  if (dtype == IMBD_BF16 && wide_pays(pass, M, N, K)) {
+    const DensePlan p = dense_wide_plan(pass, M, N, K);
+    const size_t w = range_bytes(Ranges{p.ranges, p.chunk}, M, N, db);
+    n = w > n ? w : n;
+  }
+  return n;
+}
+
 int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t s) {
   const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, N = pass == EXPERT_DW ? a.d_out : a.n_rows;
   const int K = pass == EXPERT_FWD ? a.d_in : pass == EXPERT_DX ? a.d_out : a.n_rows;
-  const Ranges r = tile_ranges(dtype, M, N, K);
+  const bool wide = wide_pays(pass, M, N, K) && dense_wide_fits(pass, dtype, a);
+  const DensePlan plan = wide ? dense_wide_plan(pass, M, N, K) : DensePlan{};
+  const Ranges r = wide ? Ranges{plan.ranges, plan.chunk} : tile_ranges(dtype, M, N, K);
+  auto run = [&](const DenseArgs &d) {
+    return wide ? run_dense_wide(pass, d, plan.bn, check, s) : run_dense_tile(pass, dtype, d, check, s);
+  };
   a.E = r.n;
   a.chunk = r.chunk;
-  if (r.n == 1) return run_dense_tile(pass, dtype, a, check, s);
+  if (r.n == 1) return run(a);
   DenseArgs part = a;
   const Partials q{reinterpret_cast<float *>(ws), partial_ld8(M), (int64_t)N * partial_ld8(M), r.n};
   float *db = reinterpret_cast<float *>(ws) + r.n * q.stride;
@@ -106,7 +125,7 @@ int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t 
   part.out_dtype = IMBD_F32;
   part.bias = nullptr;
   if (a.db) part.db = db;
-  const int rc = run_dense_tile(pass, dtype, part, check, s);
+  const int rc = run(part);
   if (rc != IMBD_OK || check) return rc;
   const int per_row = (int)(q.ld / 8);
   const int64_t rows = pass == EXPERT_DW && !a.out ? 0 : N, items = rows * per_row + (a.db ? a.d_out : 0);
@@ -136,9 +155,8 @@ DenseArgs dense_args(const LinearArgs &l) {
 }  // namespace
 
 size_t linear_ws_bytes(int which, int dtype, int d_out, int d_in, int B) {
-  if (which == 0) return range_bytes(tile_ranges(dtype, d_out, B, d_in), d_out, B, false);
-  const size_t dx = range_bytes(tile_ranges(dtype, d_in, B, d_out), d_in, B, false);
-  const size_t dw = range_bytes(tile_ranges(dtype, d_in, d_out, B), d_in, d_out, true);
+  if (which == 0) return product_bytes(EXPERT_FWD, dtype, d_out, B, d_in);
+  const size_t dx = product_bytes(EXPERT_DX, dtype, d_in, B, d_out), dw = product_bytes(EXPERT_DW, dtype, d_in, d_out, B);
   return dx > dw ? dx : dw;
 }
 
