@@ -129,6 +129,20 @@ bool dense_wide_fits(int pass, int dtype, const DenseArgs &a);
 DensePlan dense_wide_plan(int pass, int64_t M, int64_t N, int64_t K);
 int run_dense_wide(int pass, const DenseArgs &a, int bn, bool check, hipStream_t s);
 
+// Sums of ranges of K that a launch left: range s of output (n, m) at p + s*stride + (m / 64)*tile + n*ld + m % 64.
+struct DensePartials {
+  const float *p;
+  int64_t ld, tile, stride;
+  int ranges;
+};
+// Forward and Delta_X of up to 256 rows (csrc/skinny.hip): whether it takes the call, the workspace that M x N outputs need,
+// and the launch, which finishes the outputs (out->ranges == 1) or leaves its sums in ws.
+bool skinny_dense_fits(int pass, const DenseArgs &a);
+size_t skinny_dense_ws_bytes(int pass, int M, int N, int K);
+int run_skinny_dense(int pass, const DenseArgs &a, void *ws, hipStream_t s, DensePartials *out);
+// The forward product of few rows, for what dense_wide_fits takes (csrc/linear_rows.hip).
+int run_linear_rows(const DenseArgs &a, hipStream_t s);
+
 // C entry points' launches (csrc/linear.hip).
 struct LinearArgs {
   int dtype, d_out, d_in, B;

@@ -1,25 +1,20 @@
 // A fully connected layer with activation and residual, forward and backward:
 //   forward  z = W x + b, y = act(z) + r
 //   Delta_X  dx = (W^T dy) * act'(z below) + dr;   Delta_W = dy^T x, db = sum dy
-// The products run on the kernels of the expert layer (one expert that owns all rows), which finish their outputs
-// themselves where K is whole. Where their tiles are too few to fill the GPU, K is cut into ranges: each writes its fp32 sums to the
-// workspace, and linear_reduce adds them in their order and finishes the outputs the same way.
+// The products run on the kernels of the expert layer (one expert that owns all rows; csrc/expert_tile.hip and
+// csrc/linear_wide.hip), on that of small batches (csrc/skinny.hip) and on one for few rows (csrc/linear_rows.hip), which all finish
+// their outputs themselves where K is whole (dense_finish, in csrc/dense.h). Where their tiles are too few to fill the GPU, K
+// is cut into ranges: each writes its fp32 sums to the workspace, and linear_reduce adds them in their order and finishes the
+// outputs the same way.
 
 #include "dense.h"
 
 namespace imbd {
 namespace {
 
-// Sums of ranges of K: range s of output (n, m) at p + s*stride + n*ld + m.
-struct Partials {
-  const float *p;
-  int64_t ld, stride;
-  int ranges;
-};
-
 // Eight outputs of one row a thread; Delta_W's bias sums in the row after the last.
 template <typename T, int PASS>
-__global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, Partials q, const float *db, int M, int N, int per_row) {
+__global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, DensePartials q, const float *db, int M, int N, int per_row) {
   const unsigned i = blockIdx.x * 256u + threadIdx.x;
   const int n = (int)(i / (unsigned)per_row), m = 8 * (int)(i - (unsigned)n * (unsigned)per_row);
   float v[8] = {};
@@ -32,7 +27,7 @@ __global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, Partial
     return;
   }
   const int cnt = min(8, M - m);
-  const float *p = q.p + (int64_t)n * q.ld + m;  // (rows of whole eights: what is past M is not used)
+  const float *p = q.p + (int64_t)(m >> 6) * q.tile + (int64_t)n * q.ld + (m & 63);  // (whole eights: what is past M is not used)
 #pragma unroll 4
   for (int e = 0; e < q.ranges; ++e) {
     const f32x4 x = *reinterpret_cast<const f32x4 *>(p + e * q.stride), y = *reinterpret_cast<const f32x4 *>(p + e * q.stride + 4);
@@ -90,24 +85,79 @@ size_t range_bytes(const Ranges &r, int64_t M, int64_t N, bool db) {
   return r.n <= 1 ? 0 : (size_t)r.n * (size_t)(N * partial_ld8((int)M) + (db ? N : 0)) * 4;
 }
 
-// Whether the large tiles take a product that they can take: not while its rows are few (or, for Delta_W, its outputs).
-bool wide_pays(int pass, int64_t M, int64_t N, int64_t K) { return pass == EXPERT_DW ? M >= 64 && N >= 64 : N > 64; }
+// Which kernel takes a product of M x N outputs over K (rows of x and dy: N, for Delta_W K) that may have any of them (bf16,
+// rows of whole chunks). us, weights from memory.
+//  ROWS    forward of up to 16 rows (4096 x 4096, 1 / 16 rows: 9.8 / 11.3; SKINNY 13.1 / 13.3) and up to 32 while K is short (1024 x
+//          1024, 32 rows 5.4, SKINNY 6.7; 4096 x 4096 16.0 and 13.3)
+//  SKINNY  forward and Delta_X of up to 256 rows (4096 x 4096, 64 / 256 rows: forward 13.6 / 22.0, Delta_X 14.4 / 24.7; WIDE 20.6 / 30.7
+//          and 17.9 / 28.0), but for long K of many outputs (4096 outputs of 16384: forward 45.0 / 58.2, WIDE 40.3 / 57.4; Delta_X 43.1 /
+//          56.6 and 37.7 / 51.0; 1024 of 16384: 15.9 / 23.0, WIDE 25.1 / 31.5)
+//  TILE    what is too little for the large tiles, whose start and end take 8 us (forward of 2048 x 2048, 512 / 2048 rows: TILE 22.4 /
+//          36.1, WIDE 24.0 / 37.5; 1000 x 4096, 512 / 1024 rows 22.8 / 34.2 and 23.9 / 30.1. Delta_X, whose weights TILE transposes in
+//          registers: 256 x 784, 1024 / 2048 rows 8.4 / 14.4 and 8.9 / 9.2; 512 x 512, 300 rows 11.8 and 9.9. Delta_W of 1024 x 1024,
+//          512 / 1024 rows 14.8 / 31.7 and 19.3 / 24.5; 2048 x 2048, 300 / 512 rows 17.4 / 22.8 and 19.8 / 22.6)
+//  WIDE    the rest
+enum Route { ROWS, SKINNY, TILE, WIDE };
+Route route(int pass, int64_t M, int64_t N, int64_t K) {
+  const double flops = 2.0 * M * N * K;
+  if (pass == EXPERT_DW) return M * N <= (8 << 20) && (K <= 320 || flops < 1.1e9) ? TILE : WIDE;
+  if (pass == EXPERT_FWD && (N <= 16 || (N <= 32 && K <= 1024))) return ROWS;
+  if (N <= 256 && M * K < (1 << 30) - (1 << 24) && !(K > 12288 && M * K > (32 << 20))) return SKINNY;  // (32-bit offsets into W)
+  return flops < (pass == EXPERT_FWD ? 6e9 : 0.15e9) ? TILE : WIDE;
+}
 
+// The workspace of a product, whichever kernel its tensors' alignment leaves.
 size_t product_bytes(int pass, int dtype, int64_t M, int64_t N, int64_t K) {
   const bool db = pass == EXPERT_DW;
-  size_t n = range_bytes(tile_ranges(dtype, M, N, K), M, N, db);
-  if (dtype == IMBD_BF16 && wide_pays(pass, M, N, K)) {
-    const DensePlan p = dense_wide_plan(pass, M, N, K);
-    const size_t w = range_bytes(Ranges{p.ranges, p.chunk}, M, N, db);
-    n = w > n ? w : n;
+  const size_t n = range_bytes(tile_ranges(dtype, M, N, K), M, N, db);
+  if (dtype != IMBD_BF16 || M == 0 || N == 0 || K == 0) return n;
+  size_t k = 0;
+  switch (route(pass, M, N, K)) {
+    case SKINNY: k = skinny_dense_ws_bytes(pass, (int)M, (int)N, (int)K); break;
+    case WIDE: {
+      const DensePlan p = dense_wide_plan(pass, M, N, K);
+      k = range_bytes(Ranges{p.ranges, p.chunk}, M, N, db);
+      break;
+    }
+    default: break;
   }
-  return n;
+  return k > n ? k : n;
+}
+
+int reduce(int pass, int dtype, const DenseArgs &a, const DensePartials &q, const float *db, hipStream_t s) {
+  const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, N = pass == EXPERT_DW ? (a.out ? a.d_out : 0) : a.n_rows;
+  const int per_row = (int)ceil_div(M, 8);
+  const dim3 grid((unsigned)ceil_div((int64_t)N * per_row + (a.db ? a.d_out : 0), 256)), wg(256);
+  {
+    LaunchTimer t(IMBD_K_LINEAR, 3, s);
+#define GO(T)                                                                                                                 \
+  do {                                                                                                                        \
+    if (pass == EXPERT_FWD) hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_FWD>), grid, wg, 0, s, a, q, db, M, N, per_row); \
+    else if (pass == EXPERT_DX) hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_DX>), grid, wg, 0, s, a, q, db, M, N, per_row); \
+    else hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_DW>), grid, wg, 0, s, a, q, db, M, N, per_row);                   \
+  } while (0)
+    if (dtype == IMBD_BF16) GO(uint16_t);
+    else GO(float);
+#undef GO
+  }
+  return check_launch("linear_reduce");
 }
 
 int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t s) {
   const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, N = pass == EXPERT_DW ? a.d_out : a.n_rows;
   const int K = pass == EXPERT_FWD ? a.d_in : pass == EXPERT_DX ? a.d_out : a.n_rows;
-  const bool wide = wide_pays(pass, M, N, K) && dense_wide_fits(pass, dtype, a);
+  Route to = dense_wide_fits(pass, dtype, a) ? route(pass, M, N, K) : TILE;
+  if (to == SKINNY && !skinny_dense_fits(pass, a)) to = TILE;  // (past its 32-bit offsets)
+  a.E = 1;
+  a.chunk = (K + 63) / 64 * 64;
+  if (to == ROWS) return check ? IMBD_OK : run_linear_rows(a, s);
+  if (to == SKINNY) {
+    if (check) return IMBD_OK;
+    DensePartials q;
+    const int rc = run_skinny_dense(pass, a, ws, s, &q);
+    return rc != IMBD_OK || q.ranges == 1 ? rc : reduce(pass, dtype, a, q, nullptr, s);
+  }
+  const bool wide = to == WIDE;
   const DensePlan plan = wide ? dense_wide_plan(pass, M, N, K) : DensePlan{};
   const Ranges r = wide ? Ranges{plan.ranges, plan.chunk} : tile_ranges(dtype, M, N, K);
   auto run = [&](const DenseArgs &d) {
@@ -117,7 +167,7 @@ int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t 
   a.chunk = r.chunk;
   if (r.n == 1) return run(a);
   DenseArgs part = a;
-  const Partials q{reinterpret_cast<float *>(ws), partial_ld8(M), (int64_t)N * partial_ld8(M), r.n};
+  const DensePartials q{reinterpret_cast<float *>(ws), partial_ld8(M), 64, (int64_t)N * partial_ld8(M), r.n};
   float *db = reinterpret_cast<float *>(ws) + r.n * q.stride;
   part.out = pass == EXPERT_DW && !a.out ? nullptr : ws;
   part.ldo = q.ld;
@@ -126,23 +176,7 @@ int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t 
   part.bias = nullptr;
   if (a.db) part.db = db;
   const int rc = run(part);
-  if (rc != IMBD_OK || check) return rc;
-  const int per_row = (int)(q.ld / 8);
-  const int64_t rows = pass == EXPERT_DW && !a.out ? 0 : N, items = rows * per_row + (a.db ? a.d_out : 0);
-  const dim3 grid((unsigned)ceil_div(items, 256)), wg(256);
-  {
-    LaunchTimer t(IMBD_K_LINEAR, 3, s);
-#define GO(T)                                                                                                             \
-  do {                                                                                                                    \
-    if (pass == EXPERT_FWD) hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_FWD>), grid, wg, 0, s, a, q, db, M, (int)rows, per_row); \
-    else if (pass == EXPERT_DX) hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_DX>), grid, wg, 0, s, a, q, db, M, (int)rows, per_row); \
-    else hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_DW>), grid, wg, 0, s, a, q, db, M, (int)rows, per_row);         \
-  } while (0)
-    if (dtype == IMBD_BF16) GO(uint16_t);
-    else GO(float);
-#undef GO
-  }
-  return check_launch("linear_reduce");
+  return rc != IMBD_OK || check ? rc : reduce(pass, dtype, a, q, db, s);
 }
 
 DenseArgs dense_args(const LinearArgs &l) {

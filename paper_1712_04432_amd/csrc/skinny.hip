@@ -23,6 +23,7 @@
 #include <stdlib.h>
 
 #include "cdna4.h"
+#include "dense.h"
 #include "dw_wide_body.h"
 #include "local_pair.h"
 #include "loss_mean.h"
@@ -59,6 +60,11 @@ struct SkArgs {
   int b_dw4;
 };
 
+// The same for a layer with activation and residual: with K whole the kernel finishes its outputs as `d` says.
+struct SkDenseArgs : SkArgs {
+  DenseArgs d;
+};
+
 // Partial-sum layout: each workgroup's 64 x N tile is one contiguous block (a tile pitch
 // of N*64 floats plus 64, a split pitch off powers of two), so the write-out and the
 // reduce stream whole blocks.
@@ -88,8 +94,8 @@ constexpr int sk_lds_bytes() { return SK_NX * 64 * NB * 128 + SK_NW * SK_WSLOT; 
 // 16-sample blocks. One workgroup's tile: bid is its index in the launch (the product's
 // workgroups come first), smem its LDS (sk_lds_bytes<NB>() bytes). A function of its own
 // so that a launch can also run it beside another product's workgroups.
-template <bool A_TR, int NB>
-__device__ __forceinline__ void skinny_body(const SkArgs &a, char *smem, int bid) {
+template <bool A_TR, int NB, typename Args>
+__device__ __forceinline__ void skinny_body(const Args &a, char *smem, int bid) {
   constexpr uint32_t OOB = 0x80000000u;
   constexpr int XROWS = 64 * NB;
   constexpr int XSLOT = XROWS * 128;
@@ -332,7 +338,21 @@ __device__ __forceinline__ void skinny_body(const SkArgs &a, char *smem, int bid
     }
     return;
   }
-  {
+  if constexpr (std::is_same<Args, SkDenseArgs>::value) {
+    const int m = m0 + 4 * u, cnt = min(4, a.M - m);
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};
+    if (!A_TR && a.d.bias && cnt > 0) load_run(a.d.bias + m, cnt, bias);
+#pragma unroll
+    for (int p = 0; p < 2 * NB; ++p) {
+      const int nl = 32 * p + (tid >> 4), n = n0 + nl;
+      if (n >= a.N || cnt <= 0) continue;
+      const f32x4 t = *reinterpret_cast<const f32x4 *>(stg + nl * 64 + 4 * (u ^ (nl & 15)));
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = t[i] + bias[i];
+      dense_finish<uint16_t, A_TR ? EXPERT_DX : EXPERT_FWD>(a.d, n, m, cnt, v);
+    }
+  } else {
     // ---- whole K in this workgroup: out(m, n) = [mask > 0] * relu?(alpha * acc + bias[m]),
     // four consecutive m of one sample per thread, the same arithmetic as the split reduce.
     const int m = m0 + 4 * u;
@@ -397,6 +417,12 @@ __device__ __forceinline__ void skinny_body(const SkArgs &a, char *smem, int bid
 
 template <bool A_TR, int NB>
 __global__ void __launch_bounds__(512, 1) skinny_kernel(SkArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[sk_lds_bytes<NB>()];
+  skinny_body<A_TR, NB>(a, smem, (int)blockIdx.x);
+}
+
+template <bool A_TR, int NB>
+__global__ void __launch_bounds__(512, 1) skinny_dense_kernel(SkDenseArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[sk_lds_bytes<NB>()];
   skinny_body<A_TR, NB>(a, smem, (int)blockIdx.x);
 }
@@ -829,6 +855,59 @@ int run_softmax_rows_from_partials(const GemmProblem &p, const float *partial, i
     hipLaunchKernelGGL(skinny_softmax_rows, dim3(p.N), dim3(threads), 0, s, a);
   }
   return check_launch("softmax_rows_from_partials");
+}
+
+// The product of a layer with activation and residual as a problem of this kernel.
+static GemmProblem dense_problem(int pass, const DenseArgs &a) {
+  GemmProblem p;
+  p.dtype = IMBD_BF16;
+  p.A = a.w;
+  p.lda = a.ldw;
+  p.a_kc = pass == EXPERT_FWD;
+  p.B = p.a_kc ? a.x : a.dy;
+  p.ldb = p.a_kc ? a.ldx : a.lddy;
+  p.b_kc = true;
+  p.M = p.a_kc ? a.d_out : a.d_in;
+  p.N = a.n_rows;
+  p.K = p.a_kc ? a.d_in : a.d_out;
+  p.kclass = IMBD_K_LINEAR;
+  p.layer = pass;
+  return p;
+}
+
+bool skinny_dense_fits(int pass, const DenseArgs &a) { return skinny_fits(dense_problem(pass, a)); }
+
+size_t skinny_dense_ws_bytes(int pass, int M, int N, int K) {
+  GemmProblem p;
+  p.a_kc = pass == EXPERT_FWD;
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  const SkPlan pl = sk_plan(p);
+  return pl.splits == 1 ? 0 : (size_t)pl.splits * (size_t)sk_split_pitch(M, N) * sizeof(float);
+}
+
+int run_skinny_dense(int pass, const DenseArgs &a, void *ws, hipStream_t s, DensePartials *out) {
+  const GemmProblem p = dense_problem(pass, a);
+  const SkPlan pl = sk_plan(p);
+  SkDenseArgs g;
+  const int grid = prepare_skinny(p, pl, ws, false, &g);
+  g.d = a;
+  g.fused = pl.splits == 1;
+  *out = DensePartials{g.partial, 64, g.tpitch, g.sstride, pl.splits};
+  {
+    LaunchTimer t(p.kclass, p.layer, s);
+#define GO(TR)                                                                                                        \
+  do {                                                                                                                \
+    if (pl.nb == 1) hipLaunchKernelGGL((skinny_dense_kernel<TR, 1>), dim3(grid), dim3(512), 0, s, g);                 \
+    else if (pl.nb == 2) hipLaunchKernelGGL((skinny_dense_kernel<TR, 2>), dim3(grid), dim3(512), 0, s, g);            \
+    else hipLaunchKernelGGL((skinny_dense_kernel<TR, 4>), dim3(grid), dim3(512), 0, s, g);                            \
+  } while (0)
+    if (p.a_kc) GO(false);
+    else GO(true);
+#undef GO
+  }
+  return check_launch("linear_skinny");
 }
 
 size_t skinny_ws_bytes(const GemmProblem &p) {
