@@ -21,6 +21,7 @@ struct DenseArgs : ExpertArgs {
   int64_t ldz;
   const void *res;
   int64_t ldr;
+  int width;  // operands padded to whole chunks (linear.hip): the outputs' own width
 };
 
 // N consecutive elements from p on, n of them real.
@@ -128,12 +129,17 @@ struct DensePlan {
 bool dense_wide_fits(int pass, int dtype, const DenseArgs &a);
 DensePlan dense_wide_plan(int pass, int64_t M, int64_t N, int64_t K);
 int run_dense_wide(int pass, const DenseArgs &a, int bn, bool check, hipStream_t s);
+// ... of operands that are padded to whole chunks, outputs of any width and alignment (forward and Delta_X, one range)
+int run_dense_wide_any(int pass, const DenseArgs &a, int bn, bool check, hipStream_t s);
 
 // Sums of ranges of K that a launch left: range s of output (n, m) at p + s*stride + (m / 64)*tile + n*ld + m % 64.
+// Delta_W's bias sums: range s of db[o] at db + s*db_ld + o.
 struct DensePartials {
   const float *p;
   int64_t ld, tile, stride;
   int ranges;
+  const float *db;
+  int db_ld;
 };
 // Forward and Delta_X of up to 256 rows (csrc/skinny.hip): whether it takes the call, the workspace that M x N outputs need,
 // and the launch, which finishes the outputs (out->ranges == 1) or leaves its sums in ws.

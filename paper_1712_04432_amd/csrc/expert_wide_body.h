@@ -158,16 +158,70 @@ constexpr int xw_lds_bytes() {
   return (ring > stage ? ring : stage) + (xw_mask_in_lds(PASS, BN) ? BM * BN * 2 : 0);
 }
 
+// What a launch of DenseArgs does with its sums: stores them (a range's, or Delta_W), finishes them in whole chunks, or at any
+// width (DenseArgs::width) and alignment.
+enum DenseEnd { DENSE_SUMS, DENSE_CHUNKS, DENSE_ANY };
+
+// Half of a wave's sums at a time to its part of LDS in fp32, 16-byte chunks XORed with the row.
+template <int FM, int FP, int FN>
+__device__ __forceinline__ void stage_sums(f32x4 (&acc)[FM][FN], int part, uint32_t stg) {
+  constexpr int PITCH = FM * 16 * 4;
+  const int lane = threadIdx.x & 63, fi = lane & 15, kg = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const uint32_t p = stg + (uint32_t)(fi * PITCH + (((4 * i + kg) ^ fi) * 16));
+#pragma unroll
+    for (int j = 0; j < FP; ++j) {
+      f32x4 v = acc[i][part * FP + j];
+      asm volatile("" : "+a"(v));  // (read here, behind the wait states)
+      *(__attribute__((address_space(3))) f32x4 *)(uintptr_t)(p + j * 16 * PITCH) = v;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+// Eight columns of row r of what it staged.
+template <int FM>
+__device__ __forceinline__ void staged_run(uint32_t stg, int r, int ch, float (&v)[8]) {
+  const uint32_t p = stg + (uint32_t)(r * FM * 16 * 4);
+  const f32x4 lo = *(const __attribute__((address_space(3))) f32x4 *)(uintptr_t)(p + (uint32_t)(((2 * ch) ^ (r & 15)) * 16));
+  const f32x4 hi = *(const __attribute__((address_space(3))) f32x4 *)(uintptr_t)(p + (uint32_t)(((2 * ch + 1) ^ (r & 15)) * 16));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = lo[i], v[4 + i] = hi[i];
+}
+
+// Any width and alignment: eight outputs of a row a lane, as they are (dense_finish).
+template <int PASS, int FM, int FN>
+__device__ __forceinline__ void dense_any_epilogue(const DenseArgs &a, f32x4 (&acc)[FM][FN], uint32_t stg, int mw, int nw, int rows_left) {
+  constexpr int LPR = FM * 2, RPI = 64 / LPR, FP = FN / 2;  // lanes a row, rows at once
+  const int lane = threadIdx.x & 63, row0 = lane / LPR, ch = lane % LPR, m = mw + 8 * ch, cnt = min(8, a.width - m);
+  float bias[8] = {};
+  if (PASS == EXPERT_FWD && a.bias && cnt > 0) load_run(a.bias + m, cnt, bias);
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
+    stage_sums<FM, FP>(acc, part, stg);
+#pragma unroll 2
+    for (int b = 0; b < FP * 16 / RPI; ++b) {
+      const int r = b * RPI + row0, n = part * FP * 16 + r;
+      float v[8];
+      staged_run<FM>(stg, r, ch, v);
+      if (n >= rows_left || cnt <= 0) continue;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += bias[i];
+      dense_finish<uint16_t, PASS>(a, nw + n, m, cnt, v);
+    }
+  }
+}
+
 // Finishes a wave's 16 FM x 16 FN sums (dense_finish, in csrc/dense.h, on whole chunks): half its rows at a time go through
 // its part of LDS in fp32 (stg), eight columns of a row a lane come back. What the epilogue reads (the residual, the
 // activation's z) is loaded four rows' worth ahead: a wave has its SIMD for itself, nothing else hides its waits.
 template <int PASS, int ES, int FM, int FN>
 __device__ __forceinline__ void dense_wide_epilogue(const DenseArgs &a, f32x4 (&acc)[FM][FN], uint32_t stg, int mw, int nw,
                                                     int rows_left, int M) {
-  constexpr int WM = FM * 16, PITCH = WM * 4, LPR = WM / 8, RPI = 64 / LPR, FP = FN / 2;  // lanes a row, rows at once
+  constexpr int WM = FM * 16, LPR = WM / 8, RPI = 64 / LPR, FP = FN / 2;  // lanes a row, rows at once
   constexpr int NIT = FP * 16 / RPI, UN = 4;                                            // ... a half's rounds, of them together
   static_assert(NIT % UN == 0, "");
-  const int lane = threadIdx.x & 63, fi = lane & 15, kg = lane >> 4, row0 = lane / LPR, ch = lane % LPR;
+  const int lane = threadIdx.x & 63, row0 = lane / LPR, ch = lane % LPR;
   const bool in = mw + 8 * ch < M;  // (widths are multiples of 8)
   const int cols = min(WM, M - mw);
   // windows on the wave's rows, from its first column on
@@ -201,33 +255,18 @@ __device__ __forceinline__ void dense_wide_epilogue(const DenseArgs &a, f32x4 (&
   load(0, next);
 #pragma unroll
   for (int part = 0; part < 2; ++part) {
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const uint32_t p = stg + (uint32_t)(fi * PITCH + (((4 * i + kg) ^ fi) * 16));
-#pragma unroll
-      for (int j = 0; j < FP; ++j) {
-        f32x4 v = acc[i][part * FP + j];
-        asm volatile("" : "+a"(v));  // (read here, behind the wait states)
-        *(__attribute__((address_space(3))) f32x4 *)(uintptr_t)(p + j * 16 * PITCH) = v;
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    stage_sums<FM, FP>(acc, part, stg);
 #pragma unroll 1
     for (int b = 0; b < NIT / UN; ++b) {
       cur = next;
       load(part * (NIT / UN) + b + 1, next);  // (past the last: outside the window, zeros)
-      f32x4 lo[UN], hi[UN];
+      float run[UN][8];
 #pragma unroll
-      for (int q = 0; q < UN; ++q) {
-        const int r = (b * UN + q) * RPI + row0;
-        const uint32_t p = stg + (uint32_t)(r * PITCH);
-        lo[q] = *(const __attribute__((address_space(3))) f32x4 *)(uintptr_t)(p + (uint32_t)(((2 * ch) ^ (r & 15)) * 16));
-        hi[q] = *(const __attribute__((address_space(3))) f32x4 *)(uintptr_t)(p + (uint32_t)(((2 * ch + 1) ^ (r & 15)) * 16));
-      }
+      for (int q = 0; q < UN; ++q) staged_run<FM>(stg, (b * UN + q) * RPI + row0, ch, run[q]);
 #pragma unroll
       for (int q = 0; q < UN; ++q) {
         const int r = part * FP * 16 + (b * UN + q) * RPI + row0;
-        float v[8] = {lo[q][0], lo[q][1], lo[q][2], lo[q][3], hi[q][0], hi[q][1], hi[q][2], hi[q][3]};
+        float(&v)[8] = run[q];
         if constexpr (PASS == EXPERT_FWD) {
           if (use_z)
             __builtin_amdgcn_raw_buffer_store_b128(u32x4{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]),
@@ -261,9 +300,8 @@ __device__ __forceinline__ void dense_wide_epilogue(const DenseArgs &a, f32x4 (&
 }
 
 // ES: bytes of an output (a kernel for each: with both in one, the sums were copied ahead of the branch, and spilled).
-// A: ExpertArgs, or DenseArgs for one layer without experts: K in ranges, and with FINISH its own epilogue (else the fp32
-// sums of a range, or Delta_W).
-template <int PASS, int BM, int BN, bool GATHER, int ES, typename A = ExpertArgs, bool FINISH = false>
+// A: ExpertArgs, or DenseArgs for one layer without experts: K in ranges, and its own epilogue.
+template <int PASS, int BM, int BN, bool GATHER, int ES, typename A = ExpertArgs, DenseEnd END = DENSE_SUMS>
 __global__ void __launch_bounds__(256, 1) expert_wide_kernel(A a, int tiles_m, int tiles_n) {
   constexpr bool DENSE = std::is_same<A, DenseArgs>::value;
   using Sh = Shape<PASS, BM, BN>;
@@ -503,7 +541,7 @@ __global__ void __launch_bounds__(256, 1) expert_wide_kernel(A a, int tiles_m, i
   for (int i = 0; i < FM; ++i) {
     f32x4 first = {0.f, 0.f, 0.f, 0.f};
     const int m = m0 + wm * (BM / 2) + 16 * i + 4 * kg;  // (the width is a multiple of 8: all four or none)
-    if (PASS == EXPERT_FWD && a.bias && m < M)
+    if (PASS == EXPERT_FWD && END != DENSE_ANY && a.bias && m < M)
       first = *reinterpret_cast<const f32x4_any *>(a.bias + (int64_t)e * a.d_out + m);
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = first;
@@ -669,8 +707,12 @@ __global__ void __launch_bounds__(256, 1) expert_wide_kernel(A a, int tiles_m, i
   const float least = PASS == EXPERT_FWD && a.relu ? 0.f : -__builtin_inff();
   const int rows_left = min(WN, n_end - nw);
   if (rows_left <= 0 || mw >= M) return;
-  if constexpr (DENSE && FINISH) {
+  if constexpr (END == DENSE_CHUNKS) {
     dense_wide_epilogue<PASS, ES, FM, FN>(a, acc, stg, mw, nw, rows_left, M);
+    return;
+  }
+  if constexpr (END == DENSE_ANY) {
+    dense_any_epilogue<PASS, FM, FN>(a, acc, stg, mw, nw, rows_left);
     return;
   }
   // Rows of 32-bit outputs go in two halves of the wave's.

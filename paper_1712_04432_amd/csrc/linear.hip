@@ -14,7 +14,7 @@ namespace {
 
 // Eight outputs of one row a thread; Delta_W's bias sums in the row after the last.
 template <typename T, int PASS>
-__global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, DensePartials q, const float *db, int M, int N, int per_row) {
+__global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, DensePartials q, int M, int N, int per_row) {
   const unsigned i = blockIdx.x * 256u + threadIdx.x;
   const int n = (int)(i / (unsigned)per_row), m = 8 * (int)(i - (unsigned)n * (unsigned)per_row);
   float v[8] = {};
@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, DensePa
     const int o = (int)(i - (unsigned)N * (unsigned)per_row);
     if (PASS != EXPERT_DW || !a.db || o >= a.d_out) return;
     float s = 0.f;
-    for (int e = 0; e < q.ranges; ++e) s += db[(int64_t)e * a.d_out + o];
+    for (int e = 0; e < q.ranges; ++e) s += q.db[(int64_t)e * q.db_ld + o];
     a.db[o] = s;
     return;
   }
@@ -63,6 +63,24 @@ __global__ void __launch_bounds__(256) act_bwd_kernel(int act, int B, int d, con
   }
 }
 
+// dst[r][c] (ld columns, a multiple of 8) = src[r][c], zeros past its rows and columns.
+__global__ void __launch_bounds__(256) pad_kernel(const uint16_t *src, int64_t ld_src, int rows, int cols, uint16_t *dst, int ld,
+                                                  int64_t items) {
+  const int per_row = ld / 8;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per_row;
+    const int c = 8 * (int)(i - r * per_row), n = r < rows ? cols - c : 0;
+    const uint16_t *p = src + r * ld_src + c;
+    u32x4 v{};
+    if (n >= 8) v = *reinterpret_cast<const u32x4_any *>(p);
+    else
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < n) v[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
+    *reinterpret_cast<u32x4 *>(dst + i * 8) = v;
+  }
+}
+
 // ------------------------------------------------------------------------------ plans
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t partial_ld8(int M) { return ceil_div(M, 8) * 8; }
@@ -75,7 +93,7 @@ Ranges tile_ranges(int dtype, int64_t M, int64_t N, int64_t K) {
   const int64_t step = dtype == IMBD_BF16 ? 64 : 32;
   const int64_t tiles = ceil_div(M, 64) * ceil_div(N, 32);
   int64_t n = tiles > 0 ? 1024 / tiles : 1;
-  if (n > K / (8 * step)) n = K / (8 * step);
+  if (n > K / (10 * step)) n = K / (10 * step);
   if (n < 1) n = 1;
   const int64_t chunk = ceil_div(ceil_div(K, n), step) * step;
   return Ranges{(int)(K > 0 ? ceil_div(K, chunk) : 1), (int)(K > 0 ? chunk : step)};
@@ -106,12 +124,54 @@ Route route(int pass, int64_t M, int64_t N, int64_t K) {
   return flops < (pass == EXPERT_FWD ? 6e9 : 0.15e9) ? TILE : WIDE;
 }
 
+// Products of bf16 layers whose widths are no whole chunks, where it pays: on the large tiles all the same, from copies with
+// the rows padded by zeros (K too, so that no other row's elements meet them). us, padded / TILE: forward of 4099 x 4097, 64 /
+// 256 rows 37.6 / 24.3 and 45.6 / 59.1, 8192 rows 349 / 623; 2047 x 2049, 2048 / 8192 rows 58.0 / 46.7 and 94.7 / 157. Delta_X of
+// 517 x 513, 1024 / 2048 rows 21.5 / 15.2 and 23.1 / 27.9; 4099 x 4097, 64 / 8192 rows 34.6 / 42.0 and 325 / 1037. Delta_W of 1023 x
+// 1025, 512 / 1024 rows 30.1 / 27.4 and 33.4 / 45.2; 4099 x 4097, 8192 rows 397 / 1329.
+bool pads(int pass, int64_t M, int64_t N, int64_t K) {
+  const double flops = 2.0 * M * N * K;
+  if (M % 8 == 0 && (pass == EXPERT_DW ? N : K) % 8 == 0) return false;
+  if (pass == EXPERT_DW) return K >= 1024 && flops >= 2e9;
+  return flops >= (pass == EXPERT_DX ? 1e9 : K >= 4096 ? 6e9 : 2e10);
+}
+int64_t pad8(int64_t n) { return ceil_div(n, 8) * 8; }
+size_t pad_bytes(int64_t rows, int64_t cols) { return (size_t)(rows * pad8(cols) * 2 + 255) / 256 * 256; }
+bool whole_chunks(const void *p, int64_t ld, int cols) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && cols % 8 == 0 && ld < (1 << 22); }
+
+// The matrix itself, or its padded copy at *at, which moves on.
+const void *padded(const void *src, int64_t *ld, int rows, int cols, int rows_out, char **at, bool check, hipStream_t s) {
+  if (rows == rows_out && whole_chunks(src, *ld, cols)) return src;
+  uint16_t *dst = reinterpret_cast<uint16_t *>(*at);
+  const int64_t items = rows_out * (pad8(cols) / 8), blocks = ceil_div(items, 256);
+  if (!check) {
+    LaunchTimer t(IMBD_K_LINEAR, 5, s);
+    hipLaunchKernelGGL(pad_kernel, dim3((unsigned)(blocks < (1 << 16) ? blocks : 1 << 16)), dim3(256), 0, s,
+                       static_cast<const uint16_t *>(src), *ld, rows, cols, dst, (int)pad8(cols), items);
+  }
+  *at += pad_bytes(rows_out, cols);
+  *ld = pad8(cols);
+  return dst;
+}
+
 // The workspace of a product, whichever kernel its tensors' alignment leaves.
 size_t product_bytes(int pass, int dtype, int64_t M, int64_t N, int64_t K) {
   const bool db = pass == EXPERT_DW;
   const size_t n = range_bytes(tile_ranges(dtype, M, N, K), M, N, db);
   if (dtype != IMBD_BF16 || M == 0 || N == 0 || K == 0) return n;
   size_t k = 0;
+  if (pads(pass, M, N, K)) {
+    if (pass == EXPERT_DW) {
+      const DensePlan p = dense_wide_plan(pass, pad8(M), pad8(N), K);
+      k = pad_bytes(K, M) + pad_bytes(K, N) + (size_t)p.ranges * (size_t)(pad8(N) * pad8(M) + pad8(N)) * 4;
+    } else {
+      const DensePlan p = dense_wide_plan(pass, pad8(M), N, pad8(K));
+      k = pad_bytes(pad8(pass == EXPERT_FWD ? M : K), pass == EXPERT_FWD ? K : M) + pad_bytes(N, K);
+      if (p.ranges > 1) k += (size_t)p.ranges * (size_t)(N * pad8(M)) * 4;
+    }
+  }
+  const size_t padding = k > n ? k : n;
+  k = 0;
   switch (route(pass, M, N, K)) {
     case SKINNY: k = skinny_dense_ws_bytes(pass, (int)M, (int)N, (int)K); break;
     case WIDE: {
@@ -121,10 +181,10 @@ size_t product_bytes(int pass, int dtype, int64_t M, int64_t N, int64_t K) {
     }
     default: break;
   }
-  return k > n ? k : n;
+  return k > padding ? k : padding;
 }
 
-int reduce(int pass, int dtype, const DenseArgs &a, const DensePartials &q, const float *db, hipStream_t s) {
+int reduce(int pass, int dtype, const DenseArgs &a, const DensePartials &q, hipStream_t s) {
   const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, N = pass == EXPERT_DW ? (a.out ? a.d_out : 0) : a.n_rows;
   const int per_row = (int)ceil_div(M, 8);
   const dim3 grid((unsigned)ceil_div((int64_t)N * per_row + (a.db ? a.d_out : 0), 256)), wg(256);
@@ -132,9 +192,9 @@ int reduce(int pass, int dtype, const DenseArgs &a, const DensePartials &q, cons
     LaunchTimer t(IMBD_K_LINEAR, 3, s);
 #define GO(T)                                                                                                                 \
   do {                                                                                                                        \
-    if (pass == EXPERT_FWD) hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_FWD>), grid, wg, 0, s, a, q, db, M, N, per_row); \
-    else if (pass == EXPERT_DX) hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_DX>), grid, wg, 0, s, a, q, db, M, N, per_row); \
-    else hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_DW>), grid, wg, 0, s, a, q, db, M, N, per_row);                   \
+    if (pass == EXPERT_FWD) hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_FWD>), grid, wg, 0, s, a, q, M, N, per_row); \
+    else if (pass == EXPERT_DX) hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_DX>), grid, wg, 0, s, a, q, M, N, per_row); \
+    else hipLaunchKernelGGL((linear_reduce_kernel<T, EXPERT_DW>), grid, wg, 0, s, a, q, M, N, per_row);                   \
   } while (0)
     if (dtype == IMBD_BF16) GO(uint16_t);
     else GO(float);
@@ -143,10 +203,62 @@ int reduce(int pass, int dtype, const DenseArgs &a, const DensePartials &q, cons
   return check_launch("linear_reduce");
 }
 
+int padded_product(int pass, const DenseArgs &a, void *ws, bool check, hipStream_t s) {
+  char *at = static_cast<char *>(ws);
+  DenseArgs b = a;
+  b.E = 1;
+  if (pass == EXPERT_DW) {
+    if (a.out) b.x = padded(a.x, &b.ldx, a.n_rows, a.d_in, a.n_rows, &at, check, s);
+    b.dy = padded(a.dy, &b.lddy, a.n_rows, a.d_out, a.n_rows, &at, check, s);
+    b.d_in = (int)pad8(a.d_in);
+    b.d_out = (int)pad8(a.d_out);
+    const DensePlan p = dense_wide_plan(pass, b.d_in, b.d_out, a.n_rows);
+    b.E = p.ranges;
+    b.chunk = p.chunk;
+    float *sums = reinterpret_cast<float *>(at);
+    const int64_t stride = (int64_t)b.d_out * b.d_in;
+    const DensePartials q{sums, b.d_in, 64, stride, p.ranges, sums + p.ranges * stride, b.d_out};
+    b.out = a.out ? sums : nullptr;
+    b.ldo = b.d_in;
+    b.so = stride;
+    if (a.db) b.db = sums + p.ranges * stride;
+    const int rc = run_dense_wide(pass, b, p.bn, check, s);
+    return rc != IMBD_OK || check ? rc : reduce(pass, IMBD_BF16, a, q, s);
+  }
+  const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, K = pass == EXPERT_FWD ? a.d_in : a.d_out;
+  const DensePlan p = dense_wide_plan(pass, pad8(M), a.n_rows, pad8(K));
+  b.width = M;
+  if (pass == EXPERT_FWD) {  // (sums are stored in whole chunks: then W has rows for them too)
+    if (p.ranges > 1) b.d_out = (int)pad8(a.d_out);
+    b.w = padded(a.w, &b.ldw, a.d_out, a.d_in, b.d_out, &at, check, s);
+    b.x = padded(a.x, &b.ldx, a.n_rows, a.d_in, a.n_rows, &at, check, s);
+    b.d_in = (int)pad8(a.d_in);
+  } else {
+    b.d_out = (int)pad8(a.d_out);
+    b.w = padded(a.w, &b.ldw, a.d_out, a.d_in, b.d_out, &at, check, s);
+    b.dy = padded(a.dy, &b.lddy, a.n_rows, a.d_out, a.n_rows, &at, check, s);
+    b.d_in = (int)pad8(a.d_in);
+  }
+  b.E = p.ranges;
+  b.chunk = p.chunk;
+  if (p.ranges == 1) return run_dense_wide_any(pass, b, p.bn, check, s);
+  const DensePartials q{reinterpret_cast<float *>(at), pad8(M), 64, (int64_t)a.n_rows * pad8(M), p.ranges, nullptr, 0};
+  b.out = at;
+  b.ldo = q.ld;
+  b.so = q.stride;
+  b.out_dtype = IMBD_F32;
+  b.bias = nullptr;
+  const int rc = run_dense_wide(pass, b, p.bn, check, s);
+  return rc != IMBD_OK || check ? rc : reduce(pass, IMBD_BF16, a, q, s);
+}
+
 int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t s) {
   const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, N = pass == EXPERT_DW ? a.d_out : a.n_rows;
   const int K = pass == EXPERT_FWD ? a.d_in : pass == EXPERT_DX ? a.d_out : a.n_rows;
-  Route to = dense_wide_fits(pass, dtype, a) ? route(pass, M, N, K) : TILE;
+  const bool fits = dense_wide_fits(pass, dtype, a);
+  if (!fits && dtype == IMBD_BF16 && pads(pass, M, N, K) && a.n_rows < (1 << 29) && M < (1 << 22) && (pass == EXPERT_DW ? N : K) < (1 << 22))
+    return padded_product(pass, a, ws, check, s);
+  Route to = fits ? route(pass, M, N, K) : TILE;
   if (to == SKINNY && !skinny_dense_fits(pass, a)) to = TILE;  // (past its 32-bit offsets)
   a.E = 1;
   a.chunk = (K + 63) / 64 * 64;
@@ -155,7 +267,7 @@ int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t 
     if (check) return IMBD_OK;
     DensePartials q;
     const int rc = run_skinny_dense(pass, a, ws, s, &q);
-    return rc != IMBD_OK || q.ranges == 1 ? rc : reduce(pass, dtype, a, q, nullptr, s);
+    return rc != IMBD_OK || q.ranges == 1 ? rc : reduce(pass, dtype, a, q, s);
   }
   const bool wide = to == WIDE;
   const DensePlan plan = wide ? dense_wide_plan(pass, M, N, K) : DensePlan{};
@@ -167,8 +279,8 @@ int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t 
   a.chunk = r.chunk;
   if (r.n == 1) return run(a);
   DenseArgs part = a;
-  const DensePartials q{reinterpret_cast<float *>(ws), partial_ld8(M), 64, (int64_t)N * partial_ld8(M), r.n};
-  float *db = reinterpret_cast<float *>(ws) + r.n * q.stride;
+  float *db = reinterpret_cast<float *>(ws) + r.n * (int64_t)N * partial_ld8(M);
+  const DensePartials q{reinterpret_cast<float *>(ws), partial_ld8(M), 64, (int64_t)N * partial_ld8(M), r.n, db, a.d_out};
   part.out = pass == EXPERT_DW && !a.out ? nullptr : ws;
   part.ldo = q.ld;
   part.so = q.stride;
@@ -176,7 +288,7 @@ int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t 
   part.bias = nullptr;
   if (a.db) part.db = db;
   const int rc = run(part);
-  return rc != IMBD_OK || check ? rc : reduce(pass, dtype, a, q, db, s);
+  return rc != IMBD_OK || check ? rc : reduce(pass, dtype, a, q, s);
 }
 
 DenseArgs dense_args(const LinearArgs &l) {

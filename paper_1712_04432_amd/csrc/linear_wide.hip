@@ -13,7 +13,7 @@ bool al16(const void *p, int64_t ld, int es) {
   return (uintptr_t)p % 16 == 0 && ld * es % 16 == 0 && ld < ld_most;
 }
 
-template <int PASS, int BN, int ES, bool FINISH>
+template <int PASS, int BN, int ES, DenseEnd END>
 int launch(const DenseArgs &a, bool check, hipStream_t s) {
   const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in, N = PASS == EXPERT_DW ? a.d_out : a.n_rows;
   const int64_t tm = PASS == EXPERT_DW && !a.out ? 1 : (M + 255) / 256, tn = ((int64_t)N + BN - 1) / BN, blocks = a.E * tn * tm;
@@ -25,15 +25,15 @@ int launch(const DenseArgs &a, bool check, hipStream_t s) {
   const dim3 grid((unsigned)((blocks + 255) / 256 * 256));
   {
     LaunchTimer t(IMBD_K_LINEAR, PASS, s);
-    hipLaunchKernelGGL((expert_wide_kernel<PASS, 256, BN, false, ES, DenseArgs, FINISH>), grid, dim3(256), 0, s, a, (int)tm, (int)tn);
+    hipLaunchKernelGGL((expert_wide_kernel<PASS, 256, BN, false, ES, DenseArgs, END>), grid, dim3(256), 0, s, a, (int)tm, (int)tn);
   }
   return check_launch("linear_wide");
 }
 
 template <int PASS, int BN>
 int launch_rows(const DenseArgs &a, bool check, hipStream_t s) {
-  if (a.E > 1) return launch<PASS, BN, 4, false>(a, check, s);
-  return a.out_dtype == IMBD_BF16 ? launch<PASS, BN, 2, true>(a, check, s) : launch<PASS, BN, 4, true>(a, check, s);
+  if (a.E > 1) return launch<PASS, BN, 4, DENSE_SUMS>(a, check, s);
+  return a.out_dtype == IMBD_BF16 ? launch<PASS, BN, 2, DENSE_CHUNKS>(a, check, s) : launch<PASS, BN, 4, DENSE_CHUNKS>(a, check, s);
 }
 
 }  // namespace
@@ -75,7 +75,13 @@ DensePlan dense_wide_plan(int pass, int64_t M, int64_t N, int64_t K) {
 int run_dense_wide(int pass, const DenseArgs &a, int bn, bool check, hipStream_t s) {
   if (pass == EXPERT_FWD) return bn == 128 ? launch_rows<EXPERT_FWD, 128>(a, check, s) : launch_rows<EXPERT_FWD, 256>(a, check, s);
   if (pass == EXPERT_DX) return bn == 128 ? launch_rows<EXPERT_DX, 128>(a, check, s) : launch_rows<EXPERT_DX, 256>(a, check, s);
-  return launch<EXPERT_DW, 256, 4, false>(a, check, s);
+  return launch<EXPERT_DW, 256, 4, DENSE_SUMS>(a, check, s);
+}
+
+int run_dense_wide_any(int pass, const DenseArgs &a, int bn, bool check, hipStream_t s) {
+  if (pass == EXPERT_FWD)
+    return bn == 128 ? launch<EXPERT_FWD, 128, 4, DENSE_ANY>(a, check, s) : launch<EXPERT_FWD, 256, 4, DENSE_ANY>(a, check, s);
+  return bn == 128 ? launch<EXPERT_DX, 128, 4, DENSE_ANY>(a, check, s) : launch<EXPERT_DX, 256, 4, DENSE_ANY>(a, check, s);
 }
 
 }  // namespace imbd

@@ -894,7 +894,7 @@ int run_skinny_dense(int pass, const DenseArgs &a, void *ws, hipStream_t s, Dens
   const int grid = prepare_skinny(p, pl, ws, false, &g);
   g.d = a;
   g.fused = pl.splits == 1;
-  *out = DensePartials{g.partial, 64, g.tpitch, g.sstride, pl.splits};
+  *out = DensePartials{g.partial, 64, g.tpitch, g.sstride, pl.splits, nullptr, 0};
   {
     LaunchTimer t(p.kclass, p.layer, s);
 #define GO(TR)                                                                                                        \

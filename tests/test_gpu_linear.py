@@ -232,6 +232,17 @@ def test_long_sums(imbd, dev, dtype):
     _check_bwd(imbd, Layer(dev, 5, 70000, 24, dtype), "gelu_tanh")
 
 
+@pytest.mark.parametrize("B,d_out,d_in", [(2600, 2571, 2563), (2611, 2576, 2567), (2600, 2573, 2568), (5200, 1301, 2561), (40000, 1031, 129)])
+def test_wide_layers_of_odd_widths(imbd, dev, B, d_out, d_in):
+    """bf16 rows that are no whole chunks, large enough for the large tiles."""
+    L = Layer(dev, B, d_out, d_in, "bf16", pad=B % 3)
+    _check_fwd(imbd, L, "gelu_tanh")
+    _check_fwd(imbd, L, "none", bias=False, residual=False, keep=False, out="f32")
+    _check_bwd(imbd, L, "silu")
+    _check_bwd(imbd, L, "none", residual=False, out="f32", which="dx db")
+    _check_bwd(imbd, L, "gelu", in_place=True, which="dx")
+
+
 def test_no_rows(imbd, dev):
     import torch
     for dtype in ("bf16", "f32"):
