@@ -132,7 +132,7 @@ Route route(int pass, int64_t M, int64_t N, int64_t K) {
 bool pads(int pass, int64_t M, int64_t N, int64_t K) {
   const double flops = 2.0 * M * N * K;
   if (M % 8 == 0 && (pass == EXPERT_DW ? N : K) % 8 == 0) return false;
-  if (pass == EXPERT_DW) return K >= 1024 && flops >= 2e9;
+  if (pass == EXPERT_DW) return K >= 1024 && flops >= 2e9 && M * N < ((int64_t)1 << 33);  // (linear_reduce's 32-bit items)
   return flops >= (pass == EXPERT_DX ? 1e9 : K >= 4096 ? 6e9 : 2e10);
 }
 int64_t pad8(int64_t n) { return ceil_div(n, 8) * 8; }

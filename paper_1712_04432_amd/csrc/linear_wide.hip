@@ -57,7 +57,8 @@ DensePlan dense_wide_plan(int pass, int64_t M, int64_t N, int64_t K) {
   for (int bn = 128; bn <= 256; bn += 128) {
     if (pass == EXPERT_DW && bn == 128) continue;
     const int64_t tiles = tm * ((N + bn - 1) / bn);
-    for (int64_t n = 1; n <= 64 && (n == 1 || n * 4 <= slabs); ++n) {
+    // (past two rounds of workgroups more ranges only add sums)
+    for (int64_t n = 1; n <= 64 && (n == 1 || (n * 4 <= slabs && tiles * (n - 1) < 512)); ++n) {
       const int64_t per = (slabs + n - 1) / n;
       if (n > 1 && (slabs + per - 1) / per != n) continue;
       const double rounds = std::ceil((double)(tiles * n) / 256.0);
