@@ -120,6 +120,16 @@ __device__ __forceinline__ void skinny_body(const Args &a, char *smem, int bid) 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
   const uint32_t ldsx = lds0, ldsw = lds0 + XRING;
 
+  // The slab that is the S-th (those past the last are read as zeros). Rows of W a power of two apart put the same k of all of them
+  // into few of the memory's channels, so the row tiles begin at different k where the range is long (16384 x 4096, 17 / 64 rows: 35.7
+  // / 37.4 -> 32.3 / 33.2 us, weights from memory; in ranges of 1024, which begin at different k as it is, it took longer: 13.1 -> 13.9).
+  constexpr bool ROT = std::is_same<Args, SkDenseArgs>::value && !A_TR;
+  const int rot = ROT && nsl >= 32 ? __builtin_amdgcn_readfirstlane((m0 / SK_BM) % nsl) : 0;
+  auto slab = [&](int S) {
+    if constexpr (!ROT) return S;
+    const int P = S + rot;
+    return S >= nsl ? S : P >= nsl ? P - nsl : P;
+  };
   if (wave >= 6) {
     // -------------------------------------------------- activation loaders (6, 7)
     // Slab S: rows 0..XROWS-1 of the batch, k = klo + 64S ..; wave xw fills the 1 KB
@@ -175,10 +185,11 @@ __device__ __forceinline__ void skinny_body(const Args &a, char *smem, int bid) 
         kof[q] = 8 * c;
       }
       auto issue = [&](int S) {
+        const int P = slab(S);
 #pragma unroll
         for (int q = 0; q < 4 * NB; ++q) {
-          const bool ok = S * SK_KS + kof[q] < krange;
-          dma16(rb, ok ? base[q] + (uint32_t)S * 128u : OOB, dst0 + slot + q * 1024);
+          const bool ok = P * SK_KS + kof[q] < krange;
+          dma16(rb, ok ? base[q] + (uint32_t)P * 128u : OOB, dst0 + slot + q * 1024);
         }
         slot = slot + XSLOT == XRING ? 0u : slot + XSLOT;
       };
@@ -218,10 +229,11 @@ __device__ __forceinline__ void skinny_body(const Args &a, char *smem, int bid) 
     const uint32_t dst0 = ldsw + (uint32_t)(4 * lw * 1024);
     auto issue = [&](int S) {
       const uint32_t dst = dst0 + (uint32_t)((S % SK_NW) * SK_WSLOT);
+      const int P = slab(S);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const bool ok = okm[q] && S * SK_KS + kof[q] < krange;
-        dma16(ra, ok ? base[q] + (uint32_t)S * sstep : OOB, dst + q * 1024);
+        const bool ok = okm[q] && P * SK_KS + kof[q] < krange;
+        dma16(ra, ok ? base[q] + (uint32_t)P * sstep : OOB, dst + q * 1024);
       }
     };
 #pragma unroll
