@@ -12,12 +12,13 @@
 namespace imbd {
 namespace {
 
-// Eight outputs of one row a thread; Delta_W's bias sums in the row after the last.
+// RN outputs of one row a thread; Delta_W's bias sums in the row after the last.
+constexpr int RN = 4;
 template <typename T, int PASS>
 __global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, DensePartials q, int M, int N, int per_row) {
   const unsigned i = blockIdx.x * 256u + threadIdx.x;
-  const int n = (int)(i / (unsigned)per_row), m = 8 * (int)(i - (unsigned)n * (unsigned)per_row);
-  float v[8] = {};
+  const int n = (int)(i / (unsigned)per_row), m = RN * (int)(i - (unsigned)n * (unsigned)per_row);
+  float v[RN] = {};
   if (n >= N) {
     const int o = (int)(i - (unsigned)N * (unsigned)per_row);
     if (PASS != EXPERT_DW || !a.db || o >= a.d_out) return;
@@ -26,20 +27,20 @@ __global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, DensePa
     a.db[o] = s;
     return;
   }
-  const int cnt = min(8, M - m);
-  const float *p = q.p + (int64_t)(m >> 6) * q.tile + (int64_t)n * q.ld + (m & 63);  // (whole eights: what is past M is not used)
-#pragma unroll 4
+  const int cnt = min(RN, M - m);
+  const float *p = q.p + (int64_t)(m >> 6) * q.tile + (int64_t)n * q.ld + (m & 63);  // (whole fours: what is past M is not used)
+#pragma unroll 8
   for (int e = 0; e < q.ranges; ++e) {
-    const f32x4 x = *reinterpret_cast<const f32x4 *>(p + e * q.stride), y = *reinterpret_cast<const f32x4 *>(p + e * q.stride + 4);
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(p + e * q.stride);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] += x[j], v[4 + j] += y[j];
+    for (int j = 0; j < 4; ++j) v[j] += x[j];
   }
   if constexpr (PASS == EXPERT_FWD) {
     if (a.bias) {
-      float bias[8];
+      float bias[RN];
       load_run(a.bias + m, cnt, bias);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += bias[j];
+      for (int j = 0; j < RN; ++j) v[j] += bias[j];
     }
   }
   if constexpr (PASS == EXPERT_DW) {
@@ -132,7 +133,7 @@ Route route(int pass, int64_t M, int64_t N, int64_t K) {
 bool pads(int pass, int64_t M, int64_t N, int64_t K) {
   const double flops = 2.0 * M * N * K;
   if (M % 8 == 0 && (pass == EXPERT_DW ? N : K) % 8 == 0) return false;
-  if (pass == EXPERT_DW) return K >= 1024 && flops >= 2e9 && M * N < ((int64_t)1 << 33);  // (linear_reduce's 32-bit items)
+  if (pass == EXPERT_DW) return K >= 1024 && flops >= 2e9 && M * N < ((int64_t)1 << 32);  // (linear_reduce's 32-bit items)
   return flops >= (pass == EXPERT_DX ? 1e9 : K >= 4096 ? 6e9 : 2e10);
 }
 int64_t pad8(int64_t n) { return ceil_div(n, 8) * 8; }
@@ -186,7 +187,7 @@ size_t product_bytes(int pass, int dtype, int64_t M, int64_t N, int64_t K) {
 
 int reduce(int pass, int dtype, const DenseArgs &a, const DensePartials &q, hipStream_t s) {
   const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, N = pass == EXPERT_DW ? (a.out ? a.d_out : 0) : a.n_rows;
-  const int per_row = (int)ceil_div(M, 8);
+  const int per_row = (int)ceil_div(M, RN);
   const dim3 grid((unsigned)ceil_div((int64_t)N * per_row + (a.db ? a.d_out : 0), 256)), wg(256);
   {
     LaunchTimer t(IMBD_K_LINEAR, 3, s);
