@@ -127,7 +127,15 @@ struct Slope {
   }
 };
 
-// A row in a workgroup's registers: NC chunks of each of NT threads, and the last V % N elements one a thread.
+template <int NT, int N, typename TO>
+__device__ __forceinline__ void put_zero_columns(TO *out, int cols) {
+  const float zero[N] = {};
+  const int whole = cols / N, c = whole * N + (int)threadIdx.x;
+  for (int k = threadIdx.x; k < whole; k += NT) store_chunk(out + (int64_t)k * N, zero);
+  if (c < cols && c < whole * N + N) store_f32(out + c, 0.f);
+}
+
+// A row in a workgroup's registers: NC chunks of each of NT threads, and the elements of the cut chunks one a thread.
 template <typename T, int NT, int NC>
 __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a) {
   constexpr int N = chunk_elems<T>(), NW = NT / 64;
@@ -137,14 +145,11 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a) {
   const int64_t b = blockIdx.x;
   const T *z = reinterpret_cast<const T *>(a.logits) + b * a.ldz;
   T *out = a.dlogits ? reinterpret_cast<T *>(a.dlogits) + b * a.lddl : nullptr;
-  const int whole = a.V / N, rest = a.V - whole * N;
+  const RowChunks<T> row(z, a.V);
   const float w = a.weight ? a.weight[b] : 1.f;
   auto put_zeros = [&] {
     if (tid == 0) a.row_loss[b] = 0.f;
-    if (!out) return;
-    const float zero[N] = {};
-    for (int k = tid; k < whole; k += NT) store_chunk<T, N>(out + (int64_t)k * N, zero, N);
-    if (tid < rest) store_f32(out + (int64_t)whole * N + tid, 0.f);
+    if (out) put_zero_columns<NT, N>(out, a.V);
   };
   if (w == 0.f) return put_zeros();
   int id;
@@ -155,11 +160,16 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a) {
   const uint32_t fill = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int k = tid + i * NT;
+    const int k = row.first + tid + i * NT;
     v[i] = u32x4{fill, fill, fill, fill};
-    if (k < whole) v[i] = load_chunk(z + (int64_t)k * N);
+    if (k < row.whole) v[i] = row.load(k);
   }
-  const float last = tid < rest ? load_f32(z + (int64_t)whole * N + tid) : -INFINITY;
+  // threads 0 .. 15: a column of the cut chunk before the whole ones, or of that behind them
+  int column = -1;
+  if (tid < 8) column = row.skew > 0 && tid < min(N - row.skew, a.V) ? tid : -1;
+  else if (tid < 8 + N && row.tail) column = row.column(row.whole) + tid - 8;
+  if (column >= a.V) column = -1;
+  const float last = column >= 0 ? load_f32(z + column) : -INFINITY;
   const Entry e = make_entry(a, id, t, lse, room);
   if (e.none) return put_zeros();
   const float zt = e.id >= 0 && e.id < a.V ? load_f32(z + e.id) : 0.f;
@@ -191,13 +201,13 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a) {
   const Slope g(a, e, r, w);
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int k = tid + i * NT;
+    const int k = row.first + tid + i * NT;
     float d[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) d[j] = g.sq * pow2((chunk_at<T>(v[i], j) - r.m) * a.c);
-    if (k < whole) store_chunk<T, N>(out + (int64_t)k * N, d, N);
+    if (k < row.whole) store_chunk(out + row.column(k), d);
   }
-  if (tid < rest) store_f32(out + (int64_t)whole * N + tid, g.sq * pow2((last - r.m) * a.c));
+  if (column >= 0) store_f32(out + column, g.sq * pow2((last - r.m) * a.c));
   const float same = same_token(a, e, room);
   vm_barrier<0>();  // (every store of the row has landed)
   if (e.id >= 0 && e.id < a.V) store_f32(out + e.id, g.scale * (g.q1 * pow2((zt - r.m) * a.c) - same));
@@ -220,21 +230,21 @@ __global__ void __launch_bounds__(DP_NT) distill_sums_kernel(DistillArgs a) {
   }
   float best;
   int best_at;
-  const RowSums r = group_joined(walk<T, false, false>(row + c0, cols, a.c, &best, &best_at), a.c, part);
+  const RowSums r = group_joined(walk<T, false, false>(RowChunks<T>(row + c0, cols), a.c, &best, &best_at), a.c, part);
   if (tid == 0) a.sums[blockIdx.x] = r;
 }
 
 // A part of a row, of which the sums are known.
 template <typename T, typename TO>
 __global__ void __launch_bounds__(DP_NT) distill_part_kernel(DistillArgs a) {
-  constexpr int N = chunk_elems<T>(), UN = 4;
+  constexpr int N = chunk_elems<T>();
   __shared__ EntryRoom room;
   const int tid = threadIdx.x;
   const int64_t b = blockIdx.x / (unsigned)a.parts;
   const int p = (int)(blockIdx.x - b * a.parts), c0 = p * a.per, cols = min(a.per, a.V - c0);
   const T *z = reinterpret_cast<const T *>(a.logits) + b * a.ldz + c0;
   TO *out = a.dlogits ? reinterpret_cast<TO *>(a.dlogits) + b * a.lddl + c0 : nullptr;
-  const int chunks = (cols + N - 1) / N, whole = cols / N;
+  const RowChunks<T> chunks(z, cols);
   const float w = a.weight ? a.weight[b] : 1.f;
   int id;
   float t;
@@ -242,9 +252,7 @@ __global__ void __launch_bounds__(DP_NT) distill_part_kernel(DistillArgs a) {
   const Entry e = make_entry(a, id, t, a.lse ? a.lse[b] : 0.f, room);
   if (w == 0.f || e.none) {
     if (p == 0 && tid == 0) a.row_loss[b] = 0.f;
-    if (!out) return;
-    const float zero[N] = {};
-    for (int k = tid; k < chunks; k += DP_NT) store_chunk<TO, N>(out + (int64_t)k * N, zero, min(N, cols - k * N));
+    if (out) put_zero_columns<DP_NT, N>(out, cols);
     return;
   }
   const RowSums r = joined_parts(a.sums + b * a.parts, a.parts, a.c);
@@ -254,24 +262,10 @@ __global__ void __launch_bounds__(DP_NT) distill_part_kernel(DistillArgs a) {
   const bool mine = e.id >= c0 && e.id < c0 + cols;
   lds_barrier();
   const Slope g(a, e, r, w);
-  auto put = [&](const u32x4 &v, int k, int n) {
-    float d[N];
+  map_row<TO, DP_NT, WALK_UNROLL>(chunks, out, [&](const u32x4 &v, int, float(&d)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) d[i] = g.sq * pow2((chunk_at<T>(v, i) - r.m) * a.c);
-    store_chunk<TO, N>(out + (int64_t)k * N, d, n);
-  };
-  int k = tid;
-  for (; k + (UN - 1) * DP_NT < whole; k += UN * DP_NT) {
-    u32x4 v[UN];
-#pragma unroll
-    for (int q = 0; q < UN; ++q) v[q] = load_chunk(z + (int64_t)(k + q * DP_NT) * N);
-#pragma unroll
-    for (int q = 0; q < UN; ++q) put(v[q], k + q * DP_NT, N);
-  }
-  for (; k < chunks; k += DP_NT) {
-    const T *q = z + (int64_t)k * N;
-    put(k < whole ? load_chunk(q) : load_cut_chunk(q, cols - k * N), k, min(N, cols - k * N));
-  }
+  });
   const float same = same_token(a, e, room);
   vm_barrier<0>();
   if (mine) store_f32(out + (e.id - c0), g.scale * (g.q1 * pow2((zt - r.m) * a.c) - same));

@@ -92,6 +92,7 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobsArgs a) {
   const int64_t b = blockIdx.x / (unsigned)a.parts;
   const int p = (int)(blockIdx.x - b * a.parts), c0 = p * a.per, cols = min(a.per, a.V - c0);
   const T *row = reinterpret_cast<const T *>(a.logits) + b * a.ldz, *z = row + c0;
+  const RowChunks<T> chunks(z, cols);
   int t = -1;
   float zt = 0.f;
   if (a.parts == 1 && tid == 0) {
@@ -100,7 +101,7 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobsArgs a) {
   }
   float best = -INFINITY;
   int best_at = 0;
-  const RowSums r = group_joined(walk<T, ENT, TOP>(z, cols, a.c, &best, &best_at), a.c, part);
+  const RowSums r = group_joined(walk<T, ENT, TOP>(chunks, a.c, &best, &best_at), a.c, part);
   const float ls = logf(r.s);
   if (tid == 0) {
     if (a.parts == 1) put_row(a, b, r, zt, t, ls);
@@ -116,7 +117,8 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobsArgs a) {
       else a.keys[(b * a.parts + p) * a.n + j] = key;
     };
     // keys that the thread's best does reach at least, and may reach at most
-    const uint64_t some = choice_key(best, c0 + best_at * N + N - 1), most = choice_key(best, c0 + best_at * N);
+    const int at0 = chunks.column(best_at);
+    const uint64_t some = choice_key(best, c0 + at0 + N - 1), most = choice_key(best, c0 + max(at0, 0));
     keys[tid] = some;
     if (tid == 0) n_threads = n_keys = 0;
     __syncthreads();
@@ -131,33 +133,33 @@ __global__ void __launch_bounds__(LP_NT) logprobs_kernel(LogprobsArgs a) {
     const uint64_t bound = bound_of;
     if (most >= bound) threads[atomicAdd(&n_threads, 1)] = tid;
     __syncthreads();
-    // every thread looks at one chunk of one of them, several loads in flight
-    const int chunks = (cols + N - 1) / N, each = (chunks + LP_NT - 1) / LP_NT, all = n_threads * each;
+    auto look = [&](const u32x4 &v, int k) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const uint64_t key = choice_key(chunk_at<T>(v, j), c0 + chunks.column(k) + j);
+        if (key >= bound) {
+          const int at = atomicAdd(&n_keys, 1);
+          if (at < LP_LIST) keys[at] = key;
+        }
+      }
+    };
+    // every thread looks at one chunk of one of them, several loads in flight (and at the cut chunks in any case)
+    const int each = max(0, chunks.whole - chunks.first + LP_NT - 1) / LP_NT, all = n_threads * each;
     for (int i0 = tid; i0 < all; i0 += LP_UNROLL * LP_NT) {
       u32x4 v[LP_UNROLL];
       int k[LP_UNROLL];
 #pragma unroll
       for (int q = 0; q < LP_UNROLL; ++q) {
         const int i = i0 + q * LP_NT, turn = i / n_threads;
-        k[q] = i < all ? threads[i - turn * n_threads] + turn * LP_NT : chunks;
-        if (k[q] < chunks) {
-          const T *from = z + (int64_t)k[q] * N;
-          v[q] = (k[q] + 1) * N <= cols ? load_chunk(from) : load_cut_chunk(from, cols - k[q] * N);
-        }
+        k[q] = i < all ? chunks.first + threads[i - turn * n_threads] + turn * LP_NT : chunks.whole;
+        if (k[q] < chunks.whole) v[q] = chunks.load(k[q]);
       }
 #pragma unroll
-      for (int q = 0; q < LP_UNROLL; ++q) {
-        if (k[q] >= chunks) continue;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const uint64_t key = choice_key(chunk_at<T>(v[q], j), c0 + k[q] * N + j);
-          if (key >= bound) {
-            const int at = atomicAdd(&n_keys, 1);
-            if (at < LP_LIST) keys[at] = key;
-          }
-        }
-      }
+      for (int q = 0; q < LP_UNROLL; ++q)
+        if (k[q] < chunks.whole) look(v[q], k[q]);
     }
+    const bool head = chunks.skew > 0 && tid == LP_NT - 1;
+    if (head || (chunks.tail && tid == 0)) look(chunks.load_cut(head ? 0 : chunks.whole), head ? 0 : chunks.whole);
     __syncthreads();
     const int found = n_keys;
     if (found <= LP_LIST) {
@@ -222,7 +224,6 @@ struct LogprobsBwdArgs {
 template <typename T, typename TO>
 __global__ void __launch_bounds__(LP_NT) logprobs_bwd_kernel(LogprobsBwdArgs a) {
   constexpr int N = chunk_elems<T>();
-  const int tid = threadIdx.x;
   const int64_t b = blockIdx.x / (unsigned)a.parts;
   const int p = (int)(blockIdx.x - b * a.parts), c0 = p * a.per, cols = min(a.per, a.V - c0);
   const T *z = reinterpret_cast<const T *>(a.logits) + b * a.ldz + c0;
@@ -235,33 +236,18 @@ __global__ void __launch_bounds__(LP_NT) logprobs_bwd_kernel(LogprobsBwdArgs a) 
   const float lse = a.lse[b], add = h == 0.f ? 0.f : a.entropy[b];
   g *= a.inv_t;
   const float hs = h * a.inv_t, base = g + hs * add;
-  auto put = [&](const u32x4 &v, int k, int n) {
-    float d[N];
+  map_row<TO, LP_NT, LP_UNROLL>(RowChunks<T>(z, cols), out, [&](const u32x4 &v, int c, float(&d)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float lq = __builtin_elementwise_maximum(chunk_at<T>(v, i) * a.inv_t - lse, -200.f), q = pow2(lq * LOG2E);
       d[i] = -q * fmaf(hs, lq, base);
       if (none) d[i] = 0.f;
     }
-    if (at >= k * N && at < k * N + N && !none) {
+    if (at >= c && at < c + N && at >= 0 && !none) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) d[i] += k * N + i == at ? g : 0.f;
+      for (int i = 0; i < N; ++i) d[i] += c + i == at ? g : 0.f;
     }
-    store_chunk<TO, N>(out + (int64_t)k * N, d, n);
-  };
-  const int chunks = (cols + N - 1) / N, whole = cols / N;
-  int k = tid;
-  for (; k + (LP_UNROLL - 1) * LP_NT < whole; k += LP_UNROLL * LP_NT) {
-    u32x4 v[LP_UNROLL];
-#pragma unroll
-    for (int q = 0; q < LP_UNROLL; ++q) v[q] = load_chunk(z + (int64_t)(k + q * LP_NT) * N);
-#pragma unroll
-    for (int q = 0; q < LP_UNROLL; ++q) put(v[q], k + q * LP_NT, N);
-  }
-  for (; k < chunks; k += LP_NT) {
-    const T *q = z + (int64_t)k * N;
-    put(k < whole ? load_chunk(q) : load_cut_chunk(q, cols - k * N), k, min(N, cols - k * N));
-  }
+  });
 }
 
 }  // namespace

@@ -10,9 +10,9 @@ constexpr int WALK_UNROLL = 4;  // chunks of a thread in flight
 
 // One workgroup's part of a row. ENT: with u. TOP: remembers where the thread's largest logit is.
 template <typename T, bool ENT, bool TOP>
-__device__ __forceinline__ RowSums walk(const T *z, int cols, float c, float *best, int *best_at) {
+__device__ __forceinline__ RowSums walk(const RowChunks<T> &row, float c, float *best, int *best_at) {
   constexpr int N = chunk_elems<T>();
-  const int tid = threadIdx.x, chunks = (cols + N - 1) / N, whole = cols / N;
+  const int tid = threadIdx.x;
   const float slack = 16.f / c;
   RowSums r{LOWEST, 0.f, 0.f};
   auto take = [&](const auto &v, int first) {
@@ -46,17 +46,21 @@ __device__ __forceinline__ RowSums walk(const T *z, int cols, float c, float *be
       }
     }
   };
-  int k = tid;
-  for (; k + (WALK_UNROLL - 1) * WALK_NT < whole; k += WALK_UNROLL * WALK_NT) {
+  int k = row.first + tid;
+  for (; k + (WALK_UNROLL - 1) * WALK_NT < row.whole; k += WALK_UNROLL * WALK_NT) {
     u32x4 v[WALK_UNROLL];
 #pragma unroll
-    for (int q = 0; q < WALK_UNROLL; ++q) v[q] = load_chunk(z + (int64_t)(k + q * WALK_NT) * N);
+    for (int q = 0; q < WALK_UNROLL; ++q) v[q] = row.load(k + q * WALK_NT);
     take(v, k);
   }
-  for (; k < chunks; k += WALK_NT) {
-    u32x4 v[1];
-    v[0] = k < whole ? load_chunk(z + (int64_t)k * N) : load_cut_chunk(z + (int64_t)k * N, cols - k * N);
+  const bool head = row.skew > 0 && tid == WALK_NT - 1, tail = row.tail && tid == 0;
+  for (; k < row.whole; k += WALK_NT) {
+    const u32x4 v[1] = {row.load(k)};
     take(v, k);
+  }
+  if (head || tail) {
+    const u32x4 v[1] = {row.load_cut(head ? 0 : row.whole)};
+    take(v, head ? 0 : row.whole);
   }
   return r;
 }

@@ -181,6 +181,30 @@ def test_logprobs_candidates_in_one_lane(imbd, dev):
         _check_logprobs(imbd, z, _tokens(dev, 2, V), 64)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_begin_inside_a_chunk(imbd, dev, dtype):
+    """Every place in 16 bytes where a row may begin and end, short rows and rows in parts; the gradient's rows elsewhere."""
+    import torch
+    for V in (1, 2, 3, 7, 9, 15, 17, 40, 2049, 9001, 20003):
+        whole = torch.full((3 * V + 40,), float("nan"), dtype=_dt(dtype), device=dev)
+        for start in range(9):
+            z = whole[start:start + 3 * V].view(3, V)
+            z.copy_(torch.randn(3, V, generator=_gen(start, dev), device=dev) * 3)
+            tokens = _tokens(dev, 3, V)
+            _check_logprobs(imbd, z, tokens, 5)
+            ids, t = _teacher(dev, 3, V, min(V, 4))
+            _check_distill(imbd, z, ids, t, dtype)
+            g = torch.randn(3, generator=_gen(1, dev), device=dev)
+            _, ent, lse, _, _ = _run_logprobs(imbd, z, tokens, 0)
+            a = torch.full((3 * V + 9,), 7.0, dtype=_dt(dtype), device=dev)
+            b = torch.full((3, V), 7.0, dtype=_dt(dtype), device=dev)
+            imbd.token_logprobs_bwd(z, tokens, lse, a[8 - start:8 - start + 3 * V].view(3, V), dlogp=g, entropy=ent, dentropy=g)
+            imbd.token_logprobs_bwd(z.clone(), tokens, lse, b, dlogp=g, entropy=ent, dentropy=g)
+            assert torch.equal(a[8 - start:8 - start + 3 * V].view(3, V), b), (V, start)
+            assert (a[:8 - start] == 7.0).all() and (a[8 - start + 3 * V:] == 7.0).all()
+            whole.fill_(float("nan"))
+
+
 def test_logprobs_many_rows(imbd, dev):
     for dtype in ("bf16", "f32"):
         _check_logprobs(imbd, _logits(dev, 5000, 1037, dtype, "masked"), _tokens(dev, 5000, 1037), 3)
