@@ -1,7 +1,7 @@
 // Divergence of a student's softmax from a teacher of whose logits the top ones are known, and its gradient.
 //
 // Bound by memory: the logits have to be read and the gradient written. Between the two lies the softmax's sum, so
-//  * rows that fit a workgroup's registers (131072 logits in bf16, 64 registers of each of 1024 threads) stay there between
+//  * rows that fit a workgroup's registers (180224 logits in bf16, 176 registers of each of 512 threads) stay there between
 //    the sum and the gradient, and memory sees them once;
 //  * longer rows, and few rows, are cut into parts: one launch for the parts' sums, one that joins them and walks the
 //    part again.
@@ -277,16 +277,20 @@ __global__ void __launch_bounds__(256) distill_loss_kernel(int B, const float *r
 }
 
 // Chunks of a row that distill_row_kernel holds at most.
-constexpr int64_t ROW_CHUNKS_MOST = 1024 * 16;
+constexpr int64_t ROW_CHUNKS_MOST = 512 * 44;
 
 // Long rows in parts while they are fewer than CUs to fill. bf16, 131072 columns (registers / parts, the loss's launch
 // included): 8 rows 18.9 / 12.5 us, 64 21.7 / 17.7, 128 25.5 / 26.2, 512 61.8 / 70.5, 1024 134 / 170; 65536: 32 rows 13.9 / 13.3,
-// 128 16.0 / 17.6; 32768: 8 rows 11.9 / 12.2, 512 22.0 / 26.4. fp32, 65536: 32 rows 14.6 / 13.5, 64 16.6 / 16.4, 128 20.6 / 24.8.
+// 128 16.0 / 17.6; 32768: 8 rows 11.9 / 12.2, 512 22.0 / 26.4; 175000: 48 rows 28.5 / 19.8, 128 32.8 / 33.5, 512 122 / 108,
+// 1024 201 / 250. fp32, 65536: 32 rows 14.6 / 13.5, 64 16.6 / 16.4, 128 20.6 / 24.8.
 bool in_registers(int dtype, int B, int V) {
   const int64_t chunks = V / (dtype == IMBD_BF16 ? 8 : 4);
   return chunks <= 4096 || (chunks <= ROW_CHUNKS_MOST && B >= 96);
 }
 
+// Registers for both a row's logits and few idle threads: 512 threads hold 44 chunks each without spilling (48 spill).
+// bf16, 4096 rows (us): 70000 columns with 1024 threads of 16 chunks 336, with 512 of 20 252; 81920: 341, 277; 98304: 368,
+// with 512 of 24 379; 34000 to 65536 alike within 5% with 1024 of 8 and 512 of 12 or 16. 170000 in registers 617, 190000 in parts 1011.
 template <typename T>
 void launch_row(const DistillArgs &a, int B, hipStream_t s) {
   const int chunks = a.V / chunk_elems<T>();
@@ -296,7 +300,10 @@ void launch_row(const DistillArgs &a, int B, hipStream_t s) {
   else if (chunks <= 2048) GO(256, 8);
   else if (chunks <= 4096) GO(512, 8);
   else if (chunks <= 8192) GO(1024, 8);
-  else GO(1024, 16);
+  else if (chunks <= 10240) GO(512, 20);
+  else if (chunks <= 16384) GO(1024, 16);
+  else if (chunks <= 20480) GO(512, 40);
+  else GO(512, 44);
 #undef GO
 }
 

@@ -391,6 +391,15 @@ def test_distill_sizes(imbd, dev, B, V, K, dtype, out):
     _check_distill(imbd, z, ids, t, out, lse=lse, weight=weight, temperature=0.7, inv_batch=1.0 / B)
 
 
+@pytest.mark.parametrize("dtype,V", [("bf16", 70003), ("bf16", 98301), ("bf16", 150001), ("bf16", 180224), ("bf16", 180233),
+                                     ("f32", 33001), ("f32", 75003), ("f32", 90112), ("f32", 90117)])
+def test_distill_long_rows_in_registers(imbd, dev, dtype, V):
+    """Enough rows that the long ones stay in registers, up to the longest that fit and just past it."""
+    z = _logits(dev, 97, V, dtype, pad=V % 4, seed=V % 1000)
+    ids, t = _teacher(dev, 97, V, 9)
+    _check_distill(imbd, z, ids, t, dtype, temperature=0.9)
+
+
 @pytest.mark.parametrize("kind", ["masked", "lowest", "one_left", "all_lowest", "ties", "peaked", "large"])
 @pytest.mark.parametrize("B,V", [(3, 60), (2, 9001), (2, 140000), (600, 2100)])
 def test_distill_values(imbd, dev, B, V, kind):
