@@ -1,8 +1,8 @@
 """Python binding of libimbd.so: the gfx950 hot path of integrated model/batch/domain
 parallel SGD (Gholami et al., arXiv:1712.04432).
 
-Functions carry the names of the C ABI in include/imbd.h and marshal arguments (those of the
-expert layer and of AdamW also check the tensors against each other): torch tensors supply
+Functions carry the names of the C ABI in include/imbd.h and marshal arguments (those beside the
+paper's own path also check the tensors against each other): torch tensors supply
 device pointers and the current HIP stream; every step of the path runs in the library's
 kernels. Missing library -> RuntimeError (no fallback).
 

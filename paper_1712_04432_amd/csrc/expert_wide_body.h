@@ -2,7 +2,8 @@
 //   forward  y[s][o]    = sum_i W_e[o][i] x[rows[s]][i]   (+ b_e[o], ReLU)
 //   Delta_X  dx[s][i]   = sum_o W_e[o][i] dy[s][o]        (* [x > 0])
 //   Delta_W  dw_e[o][i] = sum_s dy[s][o] x[rows[s]][i];   db_e[o] = sum_s dy[s][o]
-// as D(m, n) = sum_k A(m, k) B(k, n), m the output's contiguous index (o, i, i) and n its row (s, s, o).
+// as D(m, n) = sum_k A(m, k) B(k, n), m the output's contiguous index (o, i, i) and n its row (s, s, o). With DenseArgs
+// one layer's products without experts (csrc/linear_wide.hip): "experts" are then ranges of K.
 //
 // These products are bound by the matrix cores, and the tile is chosen for what feeds them: with 128 x 128
 // outputs a wave, a k-step of 32 costs 16 KB of LDS reads and 64 matrix instructions (1024 cycles), so the

@@ -1,6 +1,7 @@
 // Forward and activation-gradient products of a fully connected layer for a batch of at
 // most 256 samples, bf16 operands (Sec. 1: Y = W X and Delta_X = W^T Delta_Y; App. A for
-// their block forms, which are the same products on a process's blocks).
+// their block forms, which are the same products on a process's blocks); also those of a layer with activation and residual
+// (skinny_dense_kernel, csrc/linear.hip).
 //
 // With B <= 256 these products stream the weight matrix once from HBM and do 2*B flops
 // per weight element. A workgroup owns a 64-row block of W against the whole batch
