@@ -120,6 +120,9 @@ __device__ __forceinline__ void dense_finish(const DenseArgs &a, int n, int m, i
 // The products' launches (one range of K or several). check: as for the expert layer's.
 // Any sizes, strides and alignments (csrc/expert_tile.hip).
 int run_dense_tile(int pass, int dtype, const DenseArgs &a, bool check, hipStream_t s);
+// ... and Delta_X and Delta_W in one launch, where both take the small tiles
+bool dense_pair_fits(int dtype, const DenseArgs &dx, const DenseArgs &dw);
+int run_dense_pair(int dtype, const DenseArgs &dx, const DenseArgs &dw, hipStream_t s);
 // bf16, rows of whole 16-byte chunks (csrc/linear_wide.hip): whether it takes the call, the plan of M x N outputs (rows
 // of a tile, ranges of K and their length, cycles), and the launch.
 struct DensePlan {

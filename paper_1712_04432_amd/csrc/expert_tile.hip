@@ -164,8 +164,10 @@ __device__ __forceinline__ bool positive(T v) {
 // TM, TN: columns (m) and rows (n) of a tile. GATHER: Delta_W with x's rows by index. (An instance for each way: with both
 // in one, fp32 Delta_W took 141 registers instead of 117 and 127, and three waves a SIMD instead of four.)
 // A: ExpertArgs, or DenseArgs for one layer without experts (K in ranges, its own epilogue).
+template <typename T, int TM, int TN>
+constexpr int TILE_LDS = 2 * (TM + TN) * XT_PITCH;
 template <typename T, int PASS, int TM, int TN, bool GATHER, typename A>
-__global__ void __launch_bounds__(256, 2) expert_tile_kernel(A a, int tiles_m, int tiles_n) {
+__device__ __forceinline__ void expert_tile(const A &a, int tiles_m, int tiles_n, unsigned block, char *smem) {
   constexpr bool DENSE = std::is_same<A, DenseArgs>::value;
   constexpr int VEC = 16 / (int)sizeof(T);
   constexpr int BK = 8 * VEC;
@@ -173,12 +175,11 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(A a, int tiles_m, i
   constexpr int FM = TM / 32, FN = TN / 32;  // 16-wide blocks of a wave (2 x 2 waves)
   constexpr int PT = TM + 4;                 // staging row pitch in floats
   static_assert(TN * PT * 4 <= 2 * STAGE, "the staged tile reuses the operand buffers");
-  __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
   // the XCDs take 32 tiles of the launch order at a time by turns (experts of different length are spread over all);
   // column tiles run fastest, so that the tiles that share rows of x (or dy) follow each other
-  const int turn = (int)(blockIdx.x >> 3), bid = ((turn >> 5) * 8 + (int)(blockIdx.x & 7)) * 32 + (turn & 31);
+  const int turn = (int)(block >> 3), bid = ((turn >> 5) * 8 + (int)(block & 7)) * 32 + (turn & 31);
   const int tm = bid % tiles_m;
   int e, n0, n_end, r0 = 0, K;
   if constexpr (PASS == EXPERT_DW) {
@@ -450,6 +451,25 @@ __global__ void __launch_bounds__(256, 2) expert_tile_kernel(A a, int tiles_m, i
   }
 }
 
+template <typename T, int PASS, int TM, int TN, bool GATHER, typename A>
+__global__ void __launch_bounds__(256, 2) expert_tile_kernel(A a, int tiles_m, int tiles_n) {
+  __shared__ __attribute__((aligned(16))) char smem[TILE_LDS<T, TM, TN>];
+  expert_tile<T, PASS, TM, TN, GATHER, A>(a, tiles_m, tiles_n, blockIdx.x, smem);
+}
+
+// A layer's two backward products in one launch: Delta_X's workgroups (dx_blocks, whole turns of the XCDs), then Delta_W's.
+struct DensePair {
+  DenseArgs dx, dw;
+  int dx_m, dx_n, dw_m, dw_n;
+  unsigned dx_blocks;
+};
+template <typename T>
+__global__ void __launch_bounds__(256, 2) linear_pair_kernel(DensePair p) {
+  __shared__ __attribute__((aligned(16))) char smem[TILE_LDS<T, 64, 32>];
+  if (blockIdx.x < p.dx_blocks) expert_tile<T, EXPERT_DX, 64, 32, false>(p.dx, p.dx_m, p.dx_n, blockIdx.x, smem);
+  else expert_tile<T, EXPERT_DW, 64, 32, false>(p.dw, p.dw_m, p.dw_n, blockIdx.x - p.dx_blocks, smem);
+}
+
 }  // namespace
 
 template <typename T, int PASS, int TM, int TN>
@@ -523,12 +543,36 @@ static int launch_dense(const DenseArgs &a, bool check, hipStream_t s) {
 
 // The larger tile by the same rule as the expert layer's, over all ranges of K.
 template <typename T, int PASS>
-static int launch_dense_sized(const DenseArgs &a, bool check, hipStream_t s) {
+static bool dense_large(const DenseArgs &a) {
   constexpr int SIDE = sizeof(T) == 2 || PASS == EXPERT_DX ? 128 : 64;
   const int M = PASS == EXPERT_FWD ? a.d_out : a.d_in, N = PASS == EXPERT_DW ? a.d_out : a.n_rows;
   const int64_t squares = (int64_t)a.E * ((M + SIDE - 1) / SIDE) * (((int64_t)N + SIDE - 1) / SIDE);
-  return squares >= (SIDE == 128 ? 256 : 1024) ? launch_dense<T, PASS, SIDE, 64>(a, check, s)
-                                              : launch_dense<T, PASS, 64, 32>(a, check, s);
+  return squares >= (SIDE == 128 ? 256 : 1024);
+}
+template <typename T, int PASS>
+static int launch_dense_sized(const DenseArgs &a, bool check, hipStream_t s) {
+  constexpr int SIDE = sizeof(T) == 2 || PASS == EXPERT_DX ? 128 : 64;
+  return dense_large<T, PASS>(a) ? launch_dense<T, PASS, SIDE, 64>(a, check, s) : launch_dense<T, PASS, 64, 32>(a, check, s);
+}
+
+template <typename T>
+static int launch_dense_pair(const DenseArgs &dx, const DenseArgs &dw, hipStream_t s) {
+  DensePair p{dx, dw, (dx.d_in + 63) / 64, (dx.n_rows + 31) / 32, dw.out ? (dw.d_in + 63) / 64 : 1, (dw.d_out + 31) / 32, 0};
+  const int64_t nx = (int64_t)dx.E * p.dx_m * p.dx_n, nw = (int64_t)dw.E * p.dw_m * p.dw_n;
+  p.dx_blocks = (unsigned)((nx + 255) / 256 * 256);
+  {
+    LaunchTimer t(IMBD_K_LINEAR, 6, s);
+    hipLaunchKernelGGL(linear_pair_kernel<T>, dim3(p.dx_blocks + (unsigned)((nw + 255) / 256 * 256)), dim3(256), 0, s, p);
+  }
+  return check_launch("linear_pair");
+}
+
+bool dense_pair_fits(int dtype, const DenseArgs &dx, const DenseArgs &dw) {
+  return dtype == IMBD_BF16 ? !dense_large<uint16_t, EXPERT_DX>(dx) && !dense_large<uint16_t, EXPERT_DW>(dw)
+                            : !dense_large<float, EXPERT_DX>(dx) && !dense_large<float, EXPERT_DW>(dw);
+}
+int run_dense_pair(int dtype, const DenseArgs &dx, const DenseArgs &dw, hipStream_t s) {
+  return dtype == IMBD_BF16 ? launch_dense_pair<uint16_t>(dx, dw, s) : launch_dense_pair<float>(dx, dw, s);
 }
 
 template <typename T>

@@ -15,8 +15,8 @@ namespace {
 // RN outputs of one row a thread; Delta_W's bias sums in the row after the last.
 constexpr int RN = 4;
 template <typename T, int PASS>
-__global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, DensePartials q, int M, int N, int per_row) {
-  const unsigned i = blockIdx.x * 256u + threadIdx.x;
+__device__ __forceinline__ void linear_reduce(const DenseArgs &a, const DensePartials &q, int M, int N, int per_row, unsigned block) {
+  const unsigned i = block * 256u + threadIdx.x;
   const int n = (int)(i / (unsigned)per_row), m = RN * (int)(i - (unsigned)n * (unsigned)per_row);
   float v[RN] = {};
   if (n >= N) {
@@ -48,6 +48,23 @@ __global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, DensePa
   } else {
     dense_finish<T, PASS>(a, n, m, cnt, v);
   }
+}
+
+template <typename T, int PASS>
+__global__ void __launch_bounds__(256) linear_reduce_kernel(DenseArgs a, DensePartials q, int M, int N, int per_row) {
+  linear_reduce<T, PASS>(a, q, M, N, per_row, blockIdx.x);
+}
+// Delta_X's and Delta_W's in one launch: the first `blocks` workgroups Delta_X's.
+struct ReducePair {
+  DenseArgs x, w;
+  DensePartials qx, qw;
+  int M, Nx, Nw, per_row;
+  unsigned blocks;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) linear_reduce_pair_kernel(ReducePair p) {
+  if (blockIdx.x < p.blocks) linear_reduce<T, EXPERT_DX>(p.x, p.qx, p.M, p.Nx, p.per_row, blockIdx.x);
+  else linear_reduce<T, EXPERT_DW>(p.w, p.qw, p.M, p.Nw, p.per_row, blockIdx.x - p.blocks);
 }
 
 template <typename T>
@@ -116,7 +133,7 @@ size_t range_bytes(const Ranges &r, int64_t M, int64_t N, bool db) {
 //          registers: 256 x 784, 1024 / 2048 rows 8.4 / 14.4 and 8.9 / 9.2; 512 x 512, 300 rows 11.8 and 9.9. Delta_W of 1024 x 1024,
 //          512 / 1024 rows 14.8 / 31.7 and 19.3 / 24.5; 2048 x 2048, 300 / 512 rows 17.4 / 22.8 and 19.8 / 22.6)
 //  WIDE    the rest
-enum Route { ROWS, SKINNY, TILE, WIDE };
+enum Route { ROWS, SKINNY, TILE, WIDE, PADDED };
 Route route(int pass, int64_t M, int64_t N, int64_t K) {
   const double flops = 2.0 * M * N * K;
   if (pass == EXPERT_DW) return M * N <= (8 << 20) && (K <= 320 || flops < 1.1e9) ? TILE : WIDE;
@@ -253,14 +270,40 @@ int padded_product(int pass, const DenseArgs &a, void *ws, bool check, hipStream
   return rc != IMBD_OK || check ? rc : reduce(pass, IMBD_BF16, a, q, s);
 }
 
-int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t s) {
+// Which kernel takes the product as its tensors lie.
+Route product_route(int pass, int dtype, const DenseArgs &a) {
   const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, N = pass == EXPERT_DW ? a.d_out : a.n_rows;
   const int K = pass == EXPERT_FWD ? a.d_in : pass == EXPERT_DX ? a.d_out : a.n_rows;
   const bool fits = dense_wide_fits(pass, dtype, a);
   if (!fits && dtype == IMBD_BF16 && pads(pass, M, N, K) && a.n_rows < (1 << 29) && M < (1 << 22) && (pass == EXPERT_DW ? N : K) < (1 << 22))
-    return padded_product(pass, a, ws, check, s);
-  Route to = fits ? route(pass, M, N, K) : TILE;
-  if (to == SKINNY && !skinny_dense_fits(pass, a)) to = TILE;  // (past its 32-bit offsets)
+    return PADDED;
+  const Route to = fits ? route(pass, M, N, K) : TILE;
+  return to == SKINNY && !skinny_dense_fits(pass, a) ? TILE : to;  // (past its 32-bit offsets)
+}
+
+// A product's arguments with its K in ranges, and where they leave their sums: from `ws` on.
+DensePartials in_ranges(int pass, const Ranges &r, DenseArgs &a, void *ws) {
+  const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, N = pass == EXPERT_DW ? a.d_out : a.n_rows;
+  a.E = r.n;
+  a.chunk = r.chunk;
+  if (r.n == 1) return DensePartials{};
+  const int64_t stride = (int64_t)N * partial_ld8(M);
+  float *db = reinterpret_cast<float *>(ws) + r.n * stride;
+  const DensePartials q{reinterpret_cast<float *>(ws), partial_ld8(M), 64, stride, r.n, db, a.d_out};
+  a.out = pass == EXPERT_DW && !a.out ? nullptr : ws;
+  a.ldo = q.ld;
+  a.so = q.stride;
+  a.out_dtype = IMBD_F32;
+  a.bias = nullptr;
+  if (a.db) a.db = db;
+  return q;
+}
+
+int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t s) {
+  const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, N = pass == EXPERT_DW ? a.d_out : a.n_rows;
+  const int K = pass == EXPERT_FWD ? a.d_in : pass == EXPERT_DX ? a.d_out : a.n_rows;
+  const Route to = product_route(pass, dtype, a);
+  if (to == PADDED) return padded_product(pass, a, ws, check, s);
   a.E = 1;
   a.chunk = (K + 63) / 64 * 64;
   if (to == ROWS) return check ? IMBD_OK : run_linear_rows(a, s);
@@ -273,23 +316,74 @@ int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t 
   const bool wide = to == WIDE;
   const DensePlan plan = wide ? dense_wide_plan(pass, M, N, K) : DensePlan{};
   const Ranges r = wide ? Ranges{plan.ranges, plan.chunk} : tile_ranges(dtype, M, N, K);
-  auto run = [&](const DenseArgs &d) {
-    return wide ? run_dense_wide(pass, d, plan.bn, check, s) : run_dense_tile(pass, dtype, d, check, s);
-  };
-  a.E = r.n;
-  a.chunk = r.chunk;
-  if (r.n == 1) return run(a);
   DenseArgs part = a;
-  float *db = reinterpret_cast<float *>(ws) + r.n * (int64_t)N * partial_ld8(M);
-  const DensePartials q{reinterpret_cast<float *>(ws), partial_ld8(M), 64, (int64_t)N * partial_ld8(M), r.n, db, a.d_out};
-  part.out = pass == EXPERT_DW && !a.out ? nullptr : ws;
-  part.ldo = q.ld;
-  part.so = q.stride;
-  part.out_dtype = IMBD_F32;
-  part.bias = nullptr;
-  if (a.db) part.db = db;
-  const int rc = run(part);
-  return rc != IMBD_OK || check ? rc : reduce(pass, dtype, a, q, s);
+  const DensePartials q = in_ranges(pass, r, part, ws);
+  const int rc = wide ? run_dense_wide(pass, part, plan.bn, check, s) : run_dense_tile(pass, dtype, part, check, s);
+  return rc != IMBD_OK || check || r.n == 1 ? rc : reduce(pass, dtype, a, q, s);
+}
+
+// Delta_X and Delta_W of a layer on the any-size kernel's small tiles in one launch, and their sums in one: starts and ends
+// overlap, and a second launch's are saved. Both are cut into ranges of L steps at most: 6 while they are too few to fill the
+// GPU's 1024 places (bf16, whose transposes take more registers: 512), 12 where they do (what is left of long ranges at
+// the end leaves CUs idle). us, in one / by themselves: rows x d_in to d_out in fp32 64 x 784 to 256 10.6 / 15.8, 300 x 512 to 512
+// 14.8 / 31.5, 1000 x 1023 to 517 49 / 55, 2048 x 1024 to 1024 122 / 161; bf16 300 x 517 to 513 15.0 / 24.4, 200 x 255 to 1001 15.3 / 30.9.
+// bf16 that has a faster kernel for one of them alone, too: 512 x 512 to 512 14.3 / 30.2, 1024 x 512 to 512 17.2 / 39.8, 1000
+// x 1024 to 512 30.8 / 42.6 (1536 x 784 to 512 47.2 / 40.7, so up to 1.15 GFLOP a product); padded copies, 1000 x 1023 to 517 45.6 /
+// 69.6, 2048 x 1023 to 517 68.9 / 77.6 (600 x 2001 to 1001 76.1 / 76.0, so up to 2.4). Not up to 256 rows on the small batches'
+// kernel: 64 x 512 to 512 12.1 / 9.7, 256 x 1024 to 1024 18.5 / 15.7.
+struct PairPlan {
+  Ranges dx, dw;
+  size_t dx_bytes, bytes;
+};
+PairPlan pair_plan(int dtype, int64_t d_out, int64_t d_in, int64_t B) {
+  const int64_t step = dtype == IMBD_BF16 ? 64 : 32;
+  const int64_t x_tiles = ceil_div(d_in, 64) * ceil_div(B, 32), w_tiles = ceil_div(d_in, 64) * ceil_div(d_out, 32);
+  const int64_t x_steps = ceil_div(d_out, step), w_steps = ceil_div(B, step);
+  const double each = ((double)x_tiles * x_steps + (double)w_tiles * w_steps) / (dtype == IMBD_BF16 ? 512 : 1024);
+  const int64_t L = each <= 6 ? 6 : each >= 12 ? 12 : (int64_t)each;
+  auto cut = [&](int64_t tiles, int64_t steps) {
+    int64_t n = dtype == IMBD_BF16 && steps <= 8 ? 1 : ceil_div(steps, L);
+    if (n > 1024 / tiles) n = 1024 / tiles;
+    if (n < 1) n = 1;
+    const int64_t len = ceil_div(steps, n);
+    return Ranges{(int)ceil_div(steps, len), (int)(len * step)};
+  };
+  PairPlan p;
+  p.dx = cut(x_tiles, x_steps);
+  p.dw = cut(w_tiles, w_steps);
+  p.dx_bytes = (range_bytes(p.dx, d_in, B, false) + 255) / 256 * 256;
+  p.bytes = p.dx_bytes + range_bytes(p.dw, d_in, d_out, true);
+  return p;
+}
+
+int reduce_pair(int dtype, const DenseArgs &x, const DenseArgs &w, const DensePartials &qx, const DensePartials &qw, hipStream_t s) {
+  ReducePair p{x, w, qx, qw, x.d_in, x.n_rows, w.out ? w.d_out : 0, (int)ceil_div(x.d_in, RN), 0};
+  p.blocks = (unsigned)ceil_div((int64_t)p.Nx * p.per_row, 256);
+  const dim3 grid(p.blocks + (unsigned)ceil_div((int64_t)p.Nw * p.per_row + (w.db ? w.d_out : 0), 256)), wg(256);
+  {
+    LaunchTimer t(IMBD_K_LINEAR, 3, s);
+    if (dtype == IMBD_BF16) hipLaunchKernelGGL(linear_reduce_pair_kernel<uint16_t>, grid, wg, 0, s, p);
+    else hipLaunchKernelGGL(linear_reduce_pair_kernel<float>, grid, wg, 0, s, p);
+  }
+  return check_launch("linear_reduce");
+}
+
+// false: not one launch's. Else *rc is the call's result.
+bool paired(int dtype, const DenseArgs &dx, const DenseArgs &dw, void *ws, hipStream_t s, int *rc) {
+  const Route to_x = product_route(EXPERT_DX, dtype, dx), to_w = product_route(EXPERT_DW, dtype, dw);
+  const double flops = 2.0 * dx.n_rows * dx.d_in * dx.d_out;
+  if (to_x == SKINNY) return false;
+  if ((to_x != TILE || to_w != TILE) && flops > (to_x == PADDED || to_w == PADDED ? 2.4e9 : 1.15e9)) return false;
+  const PairPlan p = pair_plan(dtype, dx.d_out, dx.d_in, dx.n_rows);
+  DenseArgs x = dx, w = dw;
+  const DensePartials qx = in_ranges(EXPERT_DX, p.dx, x, ws), qw = in_ranges(EXPERT_DW, p.dw, w, static_cast<char *>(ws) + p.dx_bytes);
+  if (!dense_pair_fits(dtype, x, w)) return false;
+  *rc = run_dense_pair(dtype, x, w, s);
+  if (*rc != IMBD_OK) return true;
+  if (p.dx.n > 1 && p.dw.n > 1) *rc = reduce_pair(dtype, dx, dw, qx, qw, s);
+  else if (p.dx.n > 1) *rc = reduce(EXPERT_DX, dtype, dx, qx, s);
+  else if (p.dw.n > 1) *rc = reduce(EXPERT_DW, dtype, dw, qw, s);
+  return true;
 }
 
 DenseArgs dense_args(const LinearArgs &l) {
@@ -304,7 +398,8 @@ DenseArgs dense_args(const LinearArgs &l) {
 size_t linear_ws_bytes(int which, int dtype, int d_out, int d_in, int B) {
   if (which == 0) return product_bytes(EXPERT_FWD, dtype, d_out, B, d_in);
   const size_t dx = product_bytes(EXPERT_DX, dtype, d_in, B, d_out), dw = product_bytes(EXPERT_DW, dtype, d_in, d_out, B);
-  return dx > dw ? dx : dw;
+  const size_t one = dx > dw ? dx : dw, two = B > 0 ? pair_plan(dtype, d_out, d_in, B).bytes : 0;
+  return one > two ? one : two;
 }
 
 int run_linear_fwd(const LinearArgs &l, void *ws, hipStream_t s) {
@@ -334,7 +429,9 @@ int run_linear_bwd(const LinearArgs &l, void *ws, hipStream_t s) {
     a.res = l.res; a.ldr = l.ldr;
     a.out = l.out; a.ldo = l.ldo; a.out_dtype = l.out_dtype;
     if (grad) {
-      const int rc = product(EXPERT_DW, l.dtype, g, ws, true, s);
+      int rc;
+      if (paired(l.dtype, a, g, ws, s, &rc)) return rc;
+      rc = product(EXPERT_DW, l.dtype, g, ws, true, s);
       if (rc != IMBD_OK) return rc;
     }
     const int rc = product(EXPERT_DX, l.dtype, a, ws, false, s);

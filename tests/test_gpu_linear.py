@@ -224,6 +224,19 @@ def test_parts_of_the_backward_pass(imbd, dev, B, d_out, d_in, which, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,d_out,d_in", [(64, 256, 784), (257, 8, 8), (300, 512, 512), (500, 1030, 70), (1000, 517, 1023),
+                                          (1024, 512, 560), (2100, 512, 530), (2000, 60, 33), (520, 33, 60), (700, 1501, 1100)])
+def test_both_products_of_small_layers(imbd, dev, B, d_out, d_in, dtype):
+    """Delta_X and Delta_W in one launch, K whole or in ranges for the one or the other or both; without the one or
+    the other of dw and db, the residual in place, rows apart."""
+    for pad in (0, 3):
+        L = Layer(dev, B, d_out, d_in, dtype, pad=pad, seed=B + d_out)
+        _check_bwd(imbd, L, act="gelu", out="f32")
+        _check_bwd(imbd, L, act="none", which="db dx", residual=False)
+        _check_bwd(imbd, L, act="silu", which="dw dx", in_place=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_long_sums(imbd, dev, dtype):
     """K and B that are cut into ranges, few outputs."""
     _check_fwd(imbd, Layer(dev, 3, 8, 100000, dtype), "relu")
