@@ -124,7 +124,9 @@ size_t range_bytes(const Ranges &r, int64_t M, int64_t N, bool db) {
 // Which kernel takes a product of M x N outputs over K (rows of x and dy: N, for Delta_W K) that may have any of them (bf16,
 // rows of whole chunks). us, weights from memory.
 //  ROWS    forward of up to 16 rows (4096 x 4096, 1 / 16 rows: 9.8 / 11.3; SKINNY 13.1 / 13.3) and up to 32 while K is short (1024 x
-//          1024, 32 rows 5.4, SKINNY 6.7; 4096 x 4096 16.0 and 13.3)
+//          1024, 32 rows 5.4, SKINNY 6.7; 4096 x 4096 16.0 and 13.3), but for long K, which its workgroups walk alone (1000
+//          outputs, 8 rows, K = 2048 / 4096 / 16384: ROWS 5.4 / 8.2 / 28.1, SKINNY 7.2 / 7.9 / 13.7; 2048 outputs, 4096 / 8192: 9.2 / 16.0
+//          and 9.5 / 13.1; 4096 of 8192 18.0 and 20.9, 8192 of 8192 37.5 and 36.8)
 //  SKINNY  forward and Delta_X of up to 256 rows (4096 x 4096, 64 / 256 rows: forward 13.6 / 22.0, Delta_X 14.4 / 24.7; WIDE 20.6 / 30.7
 //          and 17.9 / 28.0), but for long K of many outputs (4096 outputs of 16384: forward 45.0 / 58.2, WIDE 40.3 / 57.4; Delta_X 43.1 /
 //          56.6 and 37.7 / 51.0; 1024 of 16384: 15.9 / 23.0, WIDE 25.1 / 31.5)
@@ -137,8 +139,9 @@ enum Route { ROWS, SKINNY, TILE, WIDE, PADDED };
 Route route(int pass, int64_t M, int64_t N, int64_t K) {
   const double flops = 2.0 * M * N * K;
   if (pass == EXPERT_DW) return M * N <= (8 << 20) && (K <= 320 || flops < 1.1e9) ? TILE : WIDE;
-  if (pass == EXPERT_FWD && (N <= 16 || (N <= 32 && K <= 1024))) return ROWS;
-  if (N <= 256 && M * K < (1 << 30) - (1 << 24) && !(K > 12288 && M * K > (32 << 20))) return SKINNY;  // (32-bit offsets into W)
+  const bool near = M * K < (1 << 30) - (1 << 24);  // (SKINNY: 32-bit offsets into W)
+  if (pass == EXPERT_FWD && (N <= 16 || (N <= 32 && K <= 1024)) && (K <= 2048 || (K <= 4096 && K <= 2 * M) || !near)) return ROWS;
+  if (N <= 256 && near && !(K > 12288 && M * K > (32 << 20))) return SKINNY;
   return flops < (pass == EXPERT_FWD ? 6e9 : 0.15e9) ? TILE : WIDE;
 }
 

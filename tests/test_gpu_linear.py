@@ -236,6 +236,13 @@ def test_both_products_of_small_layers(imbd, dev, B, d_out, d_in, dtype):
         _check_bwd(imbd, L, act="silu", which="dw dx", in_place=True)
 
 
+@pytest.mark.parametrize("B,d_out,d_in", [(1, 72, 2048), (3, 264, 2056), (8, 1000, 4096), (16, 2048, 4096), (16, 2040, 4104), (5, 512, 16384)])
+def test_few_rows_of_long_sums(imbd, dev, B, d_out, d_in):
+    L = Layer(dev, B, d_out, d_in, "bf16", seed=d_in)
+    _check_fwd(imbd, L, act="gelu_tanh")
+    _check_fwd(imbd, L, keep=False, residual=False, out="f32")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_long_sums(imbd, dev, dtype):
     """K and B that are cut into ranges, few outputs."""
