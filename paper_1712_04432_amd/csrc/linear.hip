@@ -5,7 +5,7 @@
 // csrc/linear_wide.hip), on that of small batches (csrc/skinny.hip) and on one for few rows (csrc/linear_rows.hip), which all finish
 // their outputs themselves where K is whole (dense_finish, in csrc/dense.h). Where their tiles are too few to fill the GPU, K
 // is cut into ranges: each writes its fp32 sums to the workspace, and linear_reduce adds them in their order and finishes the
-// outputs the same way.
+// outputs the same way. The backward products of small layers share one launch (paired).
 
 #include "dense.h"
 
