@@ -149,8 +149,9 @@ struct DensePartials {
 bool skinny_dense_fits(int pass, const DenseArgs &a);
 size_t skinny_dense_ws_bytes(int pass, int M, int N, int K);
 int run_skinny_dense(int pass, const DenseArgs &a, void *ws, hipStream_t s, DensePartials *out);
-// The forward product of few rows, for what dense_wide_fits takes (csrc/linear_rows.hip).
-int run_linear_rows(const DenseArgs &a, hipStream_t s);
+// The forward product of up to 32 rows (csrc/linear_rows.hip), for what dense_wide_fits takes, and in fp32 for what this does.
+bool linear_rows_f32_fits(const DenseArgs &a);
+int run_linear_rows(int dtype, const DenseArgs &a, hipStream_t s);
 
 // C entry points' launches (csrc/linear.hip).
 struct LinearArgs {

@@ -136,11 +136,17 @@ size_t range_bytes(const Ranges &r, int64_t M, int64_t N, bool db) {
 //          512 / 1024 rows 14.8 / 31.7 and 19.3 / 24.5; 2048 x 2048, 300 / 512 rows 17.4 / 22.8 and 19.8 / 22.6)
 //  WIDE    the rest
 enum Route { ROWS, SKINNY, TILE, WIDE, PADDED };
+bool few_rows(int dtype, int64_t M, int64_t N, int64_t K) {
+  // (fp32 beside TILE: 8 rows, 300 x 700 4.3 / 11.0, 1000 x 2048 8.9 / 12.6, 4096 x 2048 13.3 / 18.4, 2048 x 4096 23.5 / 18.6, 8192 x 4096 35.7 /
+  // 51.8; 32 rows, 1000 x 1024 8.6 / 11.7, 4096 x 1024 10.2 / 15.5, 4096 x 2048 18.8 / 18.7, 16384 x 1000 26.1 / 24.5)
+  if (dtype == IMBD_F32) return N <= 16 ? K <= 2048 || (K <= 4096 && M >= 8192) : N <= 32 && K <= 1024 && M <= 8192;
+  return (N <= 16 || (N <= 32 && K <= 1024)) && (K <= 2048 || (K <= 4096 && K <= 2 * M));
+}
 Route route(int pass, int64_t M, int64_t N, int64_t K) {
   const double flops = 2.0 * M * N * K;
   if (pass == EXPERT_DW) return M * N <= (8 << 20) && (K <= 320 || flops < 1.1e9) ? TILE : WIDE;
   const bool near = M * K < (1 << 30) - (1 << 24);  // (SKINNY: 32-bit offsets into W)
-  if (pass == EXPERT_FWD && (N <= 16 || (N <= 32 && K <= 1024)) && (K <= 2048 || (K <= 4096 && K <= 2 * M) || !near)) return ROWS;
+  if (pass == EXPERT_FWD && (few_rows(IMBD_BF16, M, N, K) || (N <= 16 && !near))) return ROWS;
   if (N <= 256 && near && !(K > 12288 && M * K > (32 << 20))) return SKINNY;
   return flops < (pass == EXPERT_FWD ? 6e9 : 0.15e9) ? TILE : WIDE;
 }
@@ -277,8 +283,9 @@ int padded_product(int pass, const DenseArgs &a, void *ws, bool check, hipStream
 Route product_route(int pass, int dtype, const DenseArgs &a) {
   const int M = pass == EXPERT_FWD ? a.d_out : a.d_in, N = pass == EXPERT_DW ? a.d_out : a.n_rows;
   const int K = pass == EXPERT_FWD ? a.d_in : pass == EXPERT_DX ? a.d_out : a.n_rows;
+  if (dtype == IMBD_F32) return pass == EXPERT_FWD && few_rows(IMBD_F32, M, N, K) && linear_rows_f32_fits(a) ? ROWS : TILE;
   const bool fits = dense_wide_fits(pass, dtype, a);
-  if (!fits && dtype == IMBD_BF16 && pads(pass, M, N, K) && a.n_rows < (1 << 29) && M < (1 << 22) && (pass == EXPERT_DW ? N : K) < (1 << 22))
+  if (!fits && pads(pass, M, N, K) && a.n_rows < (1 << 29) && M < (1 << 22) && (pass == EXPERT_DW ? N : K) < (1 << 22))
     return PADDED;
   const Route to = fits ? route(pass, M, N, K) : TILE;
   return to == SKINNY && !skinny_dense_fits(pass, a) ? TILE : to;  // (past its 32-bit offsets)
@@ -309,7 +316,7 @@ int product(int pass, int dtype, DenseArgs a, void *ws, bool check, hipStream_t 
   if (to == PADDED) return padded_product(pass, a, ws, check, s);
   a.E = 1;
   a.chunk = (K + 63) / 64 * 64;
-  if (to == ROWS) return check ? IMBD_OK : run_linear_rows(a, s);
+  if (to == ROWS) return check ? IMBD_OK : run_linear_rows(dtype, a, s);
   if (to == SKINNY) {
     if (check) return IMBD_OK;
     DensePartials q;

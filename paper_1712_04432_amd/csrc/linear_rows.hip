@@ -1,4 +1,4 @@
-// The forward product of a fully connected layer for few rows (bf16 operands, fp32 accumulation), as a serving step makes it:
+// The forward product of a fully connected layer for few rows (bf16 or fp32, fp32 accumulation), as a serving step makes it:
 //   z[n][m] = sum_k W[m][k] x[n][k] + b[m],  y = act(z) + r
 //
 // The time is that of reading W once: nothing is staged. A wave loads its rows of W straight into the registers that the matrix
@@ -10,6 +10,7 @@
 // 8192 outputs on, where that leaves two workgroups a CU, one takes 32 of them. Weights from memory, 1 / 16 rows: 4096 x 4096
 // 9.8 / 11.3 us, 1024 x 1024 3.8 / 4.5, 16384 x 4096 32.0 / 31.9 (in 16 outputs a workgroup 31.2 / 39.2). Eight waves a workgroup (37.0
 // and 51.2 us for 4096 x 16384 instead of 33.1 and 39.9), other depths of loads and loads past the caches were no faster.
+// fp32 takes the same bytes a row in half the k: 8 rows of 4096 x 2048 13.3 us (the any-size kernel in two launches 18.4).
 
 #include "dense.h"
 
@@ -17,29 +18,29 @@ namespace imbd {
 namespace {
 
 constexpr int LR_NW = 4;                   // waves of a workgroup
-constexpr int LR_KS = 64;                  // k of a step: one line of each row
+constexpr int LR_KB = 128;                 // bytes of a step's k: one line of each row
 constexpr uint32_t LR_OOB = 0xffff0000u;   // past every descriptor
 
 // OT, NB: 16-wide blocks of outputs and of rows a workgroup. UN: steps whose loads are in flight together.
-template <int OT, int NB, int UN>
+template <typename T, int OT, int NB, int UN>
 __global__ void __launch_bounds__(LR_NW * 64) linear_rows_kernel(DenseArgs a) {
-  constexpr int OW = 16 * OT, RW = 16 * NB, PITCH = OW + 4;
+  constexpr int OW = 16 * OT, RW = 16 * NB, PITCH = OW + 4, ES = (int)sizeof(T), LR_KS = LR_KB / ES;
   __shared__ __attribute__((aligned(16))) float part[LR_NW][RW][PITCH];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int fi = lane & 15, kg = lane >> 4;
   const int m0 = (int)blockIdx.x * OW, K = a.d_in, N = a.n_rows, nsl = (K + LR_KS - 1) / LR_KS;
-  const uint16_t *w = reinterpret_cast<const uint16_t *>(a.w) + (int64_t)m0 * a.ldw;
-  const uint16_t *x = reinterpret_cast<const uint16_t *>(a.x);
+  const T *w = reinterpret_cast<const T *>(a.w) + (int64_t)m0 * a.ldw;
+  const T *x = reinterpret_cast<const T *>(a.x);
   const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint16_t *>(w), 0, (int)(uint32_t)(((int64_t)(min(OW, a.d_out - m0) - 1) * a.ldw + K) * 2), BUF_DW3);
+      const_cast<T *>(w), 0, (int)(uint32_t)(((int64_t)(min(OW, a.d_out - m0) - 1) * a.ldw + K) * ES), BUF_DW3);
   const __amdgpu_buffer_rsrc_t rx =
-      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(x), 0, (int)(uint32_t)(((int64_t)(N - 1) * a.ldx + K) * 2), BUF_DW3);
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(x), 0, (int)(uint32_t)(((int64_t)(N - 1) * a.ldx + K) * ES), BUF_DW3);
   uint32_t ow[OT], ox[NB];
 #pragma unroll
-  for (int i = 0; i < OT; ++i) ow[i] = m0 + 16 * i + fi < a.d_out ? (uint32_t)((int64_t)(16 * i + fi) * a.ldw * 2) + 16 * kg : LR_OOB;
+  for (int i = 0; i < OT; ++i) ow[i] = m0 + 16 * i + fi < a.d_out ? (uint32_t)((int64_t)(16 * i + fi) * a.ldw * ES) + 16 * kg : LR_OOB;
 #pragma unroll
-  for (int j = 0; j < NB; ++j) ox[j] = 16 * j + fi < N ? (uint32_t)((int64_t)(16 * j + fi) * a.ldx * 2) + 16 * kg : LR_OOB;
+  for (int j = 0; j < NB; ++j) ox[j] = 16 * j + fi < N ? (uint32_t)((int64_t)(16 * j + fi) * a.ldx * ES) + 16 * kg : LR_OOB;
   f32x4 acc[OT][NB];
 #pragma unroll
   for (int i = 0; i < OT; ++i)
@@ -54,8 +55,8 @@ __global__ void __launch_bounds__(LR_NW * 64) linear_rows_kernel(DenseArgs a) {
     for (int u = 0; u < UN; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const bool in = !CUT || (S + u < s1 && (S + u) * LR_KS + 32 * h + 8 * kg < K);
-        const uint32_t k2 = (uint32_t)((S + u) * LR_KS + 32 * h) * 2;
+        const bool in = !CUT || (S + u < s1 && (S + u) * LR_KS + (64 * h + 16 * kg) / ES < K);
+        const uint32_t k2 = (uint32_t)(S + u) * LR_KB + 64 * h;
 #pragma unroll
         for (int i = 0; i < OT; ++i)
           wv[u][h][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, in ? ow[i] : LR_OOB, in ? k2 : 0, 0));
@@ -70,9 +71,16 @@ __global__ void __launch_bounds__(LR_NW * 64) linear_rows_kernel(DenseArgs a) {
 #pragma unroll
         for (int i = 0; i < OT; ++i)
 #pragma unroll
-          for (int j = 0; j < NB; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv[u][h][i]),
-                                                                __builtin_bit_cast(bf16x8, xv[u][h][j]), acc[i][j], 0, 0, 0);
+          for (int j = 0; j < NB; ++j) {
+            if constexpr (ES == 2) {
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv[u][h][i]),
+                                                                  __builtin_bit_cast(bf16x8, xv[u][h][j]), acc[i][j], 0, 0, 0);
+            } else {  // (the four lanes of a row each hold four k in a row: an instruction takes the q-th of each)
+              const f32x4 wf = __builtin_bit_cast(f32x4, wv[u][h][i]), xf = __builtin_bit_cast(f32x4, xv[u][h][j]);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(wf[q], xf[q], acc[i][j], 0, 0, 0);
+            }
+          }
   };
   int S = s0;
   for (; S + UN <= s1 && (S + UN) * LR_KS <= K; S += UN) steps(S, std::integral_constant<bool, false>{});
@@ -96,11 +104,11 @@ __global__ void __launch_bounds__(LR_NW * 64) linear_rows_kernel(DenseArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] += bias[i];
     }
-    dense_finish<uint16_t, EXPERT_FWD>(a, n, m, cnt, v);
+    dense_finish<T, EXPERT_FWD>(a, n, m, cnt, v);
   }
 }
 
-template <int OT, int NB, int UN>
+template <typename T, int OT, int NB, int UN>
 int launch(const DenseArgs &a, hipStream_t s) {
   const int tm = (a.d_out + 16 * OT - 1) / (16 * OT);
   if (tm > WORKGROUPS_MOST) {
@@ -109,16 +117,26 @@ int launch(const DenseArgs &a, hipStream_t s) {
   }
   {
     LaunchTimer t(IMBD_K_LINEAR, EXPERT_FWD, s);
-    hipLaunchKernelGGL((linear_rows_kernel<OT, NB, UN>), dim3((unsigned)tm), dim3(LR_NW * 64), 0, s, a);
+    hipLaunchKernelGGL((linear_rows_kernel<T, OT, NB, UN>), dim3((unsigned)tm), dim3(LR_NW * 64), 0, s, a);
   }
   return check_launch("linear_rows");
 }
 
+template <typename T>
+int launch_sized(const DenseArgs &a, hipStream_t s) {
+  if (a.n_rows > 16) return a.d_out >= 8192 ? launch<T, 2, 2, 2>(a, s) : launch<T, 1, 2, 2>(a, s);
+  return a.d_out >= 8192 ? launch<T, 2, 1, 4>(a, s) : launch<T, 1, 1, 4>(a, s);
+}
+
 }  // namespace
 
-int run_linear_rows(const DenseArgs &a, hipStream_t s) {
-  if (a.n_rows > 16) return a.d_out >= 8192 ? launch<2, 2, 2>(a, s) : launch<1, 2, 2>(a, s);
-  return a.d_out >= 8192 ? launch<2, 1, 4>(a, s) : launch<1, 1, 4>(a, s);
+bool linear_rows_f32_fits(const DenseArgs &a) {
+  auto fits = [](const void *p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 4 == 0 && ld < (1 << 22); };
+  return a.d_in % 4 == 0 && fits(a.w, a.ldw) && fits(a.x, a.ldx);
+}
+
+int run_linear_rows(int dtype, const DenseArgs &a, hipStream_t s) {
+  return dtype == IMBD_BF16 ? launch_sized<uint16_t>(a, s) : launch_sized<float>(a, s);
 }
 
 }  // namespace imbd

@@ -243,6 +243,15 @@ def test_few_rows_of_long_sums(imbd, dev, B, d_out, d_in):
     _check_fwd(imbd, L, keep=False, residual=False, out="f32")
 
 
+@pytest.mark.parametrize("pad", [0, 3, 4])
+@pytest.mark.parametrize("B,d_out,d_in", [(1, 72, 2048), (1, 5, 4), (9, 264, 1028), (16, 8200, 2052), (17, 33, 36), (32, 1000, 1024), (31, 8209, 20),
+                                          (4, 8192, 4096)])
+def test_few_rows_in_single_precision(imbd, dev, B, d_out, d_in, pad):
+    L = Layer(dev, B, d_out, d_in, "f32", pad=pad, seed=d_in)
+    _check_fwd(imbd, L, act="gelu")
+    _check_fwd(imbd, L, keep=False, bias=False, out="bf16", in_place=True)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_long_sums(imbd, dev, dtype):
     """K and B that are cut into ranges, few outputs."""
