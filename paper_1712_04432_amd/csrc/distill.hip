@@ -283,9 +283,10 @@ constexpr int64_t ROW_CHUNKS_MOST = 512 * 44;
 // included): 8 rows 18.9 / 12.5 us, 64 21.7 / 17.7, 128 25.5 / 26.2, 512 61.8 / 70.5, 1024 134 / 170; 65536: 32 rows 13.9 / 13.3,
 // 128 16.0 / 17.6; 32768: 8 rows 11.9 / 12.2, 512 22.0 / 26.4; 175000: 48 rows 28.5 / 19.8, 128 32.8 / 33.5, 512 122 / 108,
 // 1024 201 / 250. fp32, 65536: 32 rows 14.6 / 13.5, 64 16.6 / 16.4, 128 20.6 / 24.8.
+// (A launch holds fewer than 2^32 work-items, which rows of more than 256 threads can pass: those in parts have 256.)
 bool in_registers(int dtype, int B, int V) {
-  const int64_t chunks = V / (dtype == IMBD_BF16 ? 8 : 4);
-  return chunks <= 4096 || (chunks <= ROW_CHUNKS_MOST && B >= 96);
+  const int64_t chunks = V / (dtype == IMBD_BF16 ? 8 : 4), threads = chunks <= 2048 ? 256 : chunks <= 4096 ? 512 : 1024;
+  return (chunks <= 4096 || (chunks <= ROW_CHUNKS_MOST && B >= 96)) && B * threads < (int64_t)1 << 32;
 }
 
 // Registers for both a row's logits and few idle threads: 512 threads hold 44 chunks each without spilling (48 spill).

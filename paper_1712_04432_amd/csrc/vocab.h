@@ -11,7 +11,7 @@ constexpr int TOP_MOST = 64;         // alternatives
 constexpr int ENTRIES_MOST = 256;    // a teacher's entries of a row
 constexpr int PARTS_MOST = 32;      // of a row
 constexpr int VOCAB_MOST = 1 << 30;
-constexpr int VOCAB_ROWS_MOST = (1 << 24) - 1;  // a workgroup each: 2^32 work-items are a launch's most
+constexpr int VOCAB_ROWS_MOST = (1 << 24) - 1;  // a workgroup of 256 each: a launch holds fewer than 2^32 work-items
 
 size_t logprobs_ws_bytes(int B, int V, int n);
 int run_logprobs(int dtype, int B, int V, int n, const void *logits, int64_t ldz, const int32_t *tokens,
