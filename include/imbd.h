@@ -535,7 +535,8 @@ enum imbd_kernel_class {
     IMBD_K_CONV_FWD = 8, IMBD_K_CONV_DGRAD = 9, IMBD_K_CONV_WGRAD = 10,
     IMBD_K_EXPERT_FWD = 11, IMBD_K_EXPERT_DX = 12, IMBD_K_EXPERT_DW = 13,
     IMBD_K_ROUTE = 14, IMBD_K_COMBINE = 15, IMBD_K_ADAMW = 16, IMBD_K_DISTILL = 17,
-    IMBD_K_LOGPROBS = 18, IMBD_K_LINEAR = 19
+    IMBD_K_LOGPROBS = 18, IMBD_K_LINEAR = 19,
+    IMBD_K_COUNT = 20
 };
 /* Start recording HIP events around every launch of kernel class `cls` whose layer tag
  * equals `layer` (-1: any layer), up to max_launches launches. Creates the events

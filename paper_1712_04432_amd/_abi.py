@@ -21,6 +21,7 @@ IMBD_ACT_NONE, IMBD_ACT_RELU, IMBD_ACT_GELU, IMBD_ACT_GELU_TANH, IMBD_ACT_SILU =
  IMBD_K_SGD, IMBD_K_CAST, IMBD_K_CONV_FWD, IMBD_K_CONV_DGRAD, IMBD_K_CONV_WGRAD, IMBD_K_EXPERT_FWD,
  IMBD_K_EXPERT_DX, IMBD_K_EXPERT_DW, IMBD_K_ROUTE, IMBD_K_COMBINE, IMBD_K_ADAMW, IMBD_K_DISTILL, IMBD_K_LOGPROBS,
  IMBD_K_LINEAR) = range(20)
+IMBD_K_COUNT = 20
 
 # every function the header declares: name -> (restype, argtypes)
 _i, _l, _p, _f, _d, _z = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_double, ctypes.c_size_t

@@ -702,7 +702,7 @@ int conv3x3_tile_bwd(int N, int H, int W, int C_in, int C_out, const void *x_pad
 int imbd_timing_begin(int cls, int layer, int max_launches) {
   std::lock_guard<std::mutex> lk(g_timing.mu);
   if (g_timing.active) FAIL(IMBD_EINVAL, "a timing recording is already open");
-  if (cls < 0 || cls > IMBD_K_ADAMW || max_launches < 1 || max_launches > 100000)
+  if (cls < 0 || cls >= IMBD_K_COUNT || max_launches < 1 || max_launches > 100000)
     FAIL(IMBD_EINVAL, "bad timing request");
   g_timing.ev.assign(2 * (size_t)max_launches, nullptr);
   for (auto &e : g_timing.ev)
