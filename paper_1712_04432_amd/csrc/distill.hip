@@ -355,7 +355,10 @@ int run_distill(int dtype, int B, int V, int K, const void *logits, int64_t ldz,
     }
     if (rc != IMBD_OK) return rc;
   }
-  hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(256), 0, s, B, row_loss, inv_batch, loss);
+  {
+    LaunchTimer t(IMBD_K_DISTILL, 2, s);
+    hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(256), 0, s, B, row_loss, inv_batch, loss);
+  }
   return check_launch("distill_xent (loss)");
 }
 
