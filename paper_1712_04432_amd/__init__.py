@@ -37,7 +37,8 @@ __all__ = [
     "timing_end",
     "expert_route_workspace_bytes", "expert_route", "expert_route_bwd", "expert_fwd", "expert_bwd",
     "expert_combine", "expert_combine_bwd", "AdamW", "adamw_step",
-    "linear_workspace_bytes", "linear_fwd", "linear_bwd", "act_bwd", "distill_workspace_bytes", "distill_xent", "token_logprobs_workspace_bytes", "token_logprobs", "token_logprobs_bwd",
+    "linear_workspace_bytes", "linear_fwd", "linear_bwd", "act_bwd", "distill_workspace_bytes", "distill_xent",
+    "token_logprobs_workspace_bytes", "token_logprobs", "token_logprobs_bwd",
     "ws_view", "dtype_code", "set_option", "get_option", "option_name", "options",
 ]
 

@@ -10,8 +10,9 @@ __device__ __forceinline__ float quick_exp(float x) { return __builtin_amdgcn_ex
 __device__ __forceinline__ float quick_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
 
 // The standard normal distribution's tail beyond u >= 0, given e = exp(-u^2 / 2): e times a rational function of u, whose
-// coefficients are a least-maximum fit of exp(u^2 / 2) * tail in t = 1 / (1 + u / 4) over all u (relative error 3.4e-8, 1.6e-7
-// as evaluated in fp32), so that the tail is exact relatively however small it is.
+// coefficients are a least-maximum fit of exp(u^2 / 2) * tail in t = 1 / (1 + u / 4) over all u (relative error 4.7e-8 with the
+// coefficients as rounded, 4e-7 as evaluated in fp32; tests/test_act_fit.py). Nothing cancels, so the tail keeps its
+// digits however small it is but for those that e loses to its argument's rounding: its relative error grows as 2^-24 u^2.
 __device__ __forceinline__ float normal_tail(float u, float e) {
   const float t = quick_rcp(fmaf(0.25f, u, 1.f));
   float p = 0.0197819881f;

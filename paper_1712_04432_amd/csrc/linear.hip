@@ -12,7 +12,8 @@
 namespace imbd {
 namespace {
 
-// RN outputs of one row a thread; Delta_W's bias sums in the row after the last.
+// RN outputs of one row a thread; Delta_W's bias sums in the row after the last. (bf16 outputs: 4 ranges of 64 x 4096 3.8 us, 3 of 512
+// x 4096 6.5, 4.5 TB/s of what the product has just left in the caches.)
 constexpr int RN = 4;
 template <typename T, int PASS>
 __device__ __forceinline__ void linear_reduce(const DenseArgs &a, const DensePartials &q, int M, int N, int per_row, unsigned block) {
@@ -67,6 +68,8 @@ __global__ void __launch_bounds__(256) linear_reduce_pair_kernel(ReducePair p) {
   else linear_reduce<T, EXPERT_DW>(p.w, p.qw, p.M, p.Nw, p.per_row, blockIdx.x - p.blocks);
 }
 
+// Three tensors once. bf16, 8192 x 16384: silu 139 us (5.8 TB/s), bound by memory; gelu, with more arithmetic an element, 189; 64 x
+// 4096 3.2 us.
 template <typename T>
 __global__ void __launch_bounds__(256) act_bwd_kernel(int act, int B, int d, const T *dy, int64_t lddy, const T *z, int64_t ldz,
                                                       T *dz, int64_t lddz, int64_t items, int per_row) {
@@ -126,7 +129,10 @@ size_t range_bytes(const Ranges &r, int64_t M, int64_t N, bool db) {
 //  ROWS    forward of up to 16 rows (4096 x 4096, 1 / 16 rows: 9.8 / 11.3; SKINNY 13.1 / 13.3) and up to 32 while K is short (1024 x
 //          1024, 32 rows 5.4, SKINNY 6.7; 4096 x 4096 16.0 and 13.3), but for long K, which its workgroups walk alone (1000
 //          outputs, 8 rows, K = 2048 / 4096 / 16384: ROWS 5.4 / 8.2 / 28.1, SKINNY 7.2 / 7.9 / 13.7; 2048 outputs, 4096 / 8192: 9.2 / 16.0
-//          and 9.5 / 13.1; 4096 of 8192 18.0 and 20.9, 8192 of 8192 37.5 and 36.8)
+//          and 9.5 / 13.1; 4096 of 8192 18.0 and 20.9, 8192 of 8192 37.5 and 36.8). Up to 16 rows of weights past SKINNY's offsets (2^30
+//          elements, 2.1 GB) go here at any K: 65536 outputs of 16384, 1 / 8 / 16 rows 411 / 433 / 474 (WIDE, 17 rows, 378), 16384 of
+//          65536 357 / 360 / 430 (401), 4096 of 262144 394 / 428 / 497 (398); few outputs of very long K are slower here than they would
+//          be in WIDE's ranges (1024 of 1048576 1528 / 2062 / 3130, and 591)
 //  SKINNY  forward and Delta_X of up to 256 rows (4096 x 4096, 64 / 256 rows: forward 13.6 / 22.0, Delta_X 14.4 / 24.7; WIDE 20.6 / 30.7
 //          and 17.9 / 28.0), but for long K of many outputs (4096 outputs of 16384: forward 45.0 / 58.2, WIDE 40.3 / 57.4; Delta_X 43.1 /
 //          56.6 and 37.7 / 51.0; 1024 of 16384: 15.9 / 23.0, WIDE 25.1 / 31.5)
